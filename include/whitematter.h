@@ -91,8 +91,14 @@ enum wm_op {
   WM_OP_Q_BACKWARD = 10,      /* wm_q_project_backward */
   WM_OP_POOL_BACKWARD = 11,   /* wm_pool_backward */
   WM_OP_STEP_BACKWARD = 12,   /* wm_layer_step_backward */
-  WM_OP_PASSES_BACKWARD = 13  /* wm_prefill_passes_backward (size: see
+  WM_OP_PASSES_BACKWARD = 13, /* wm_prefill_passes_backward (size: see
                                  wm_passes_backward_workspace) */
+  WM_OP_WINDOW_ATTEND = 14,   /* wm_channel_attend_window */
+  WM_OP_WINDOW_BACKWARD = 15, /* wm_channel_attend_window_backward */
+  WM_OP_SHARED_ATTEND = 16,   /* wm_channel_attend_shared (size: see wm_shared_workspace) */
+  WM_OP_WEIGH_ATTEND = 17,    /* wm_channel_attend_weigh */
+  WM_OP_CACHE_EVICT = 18,     /* wm_cache_evict */
+  WM_OP_PREFIX_SHARE = 19     /* wm_prefix_share (no workspace) */
 };
 
 /* Problem dimensions (paper notation). Supported: 1 <= L <= 64, 1 <= k <= L,
@@ -449,6 +455,107 @@ int wm_prefill_passes_backward(const wm_dims *dims, const wm_params *params, con
 /* Bytes of workspace wm_prefill_passes_backward needs for a window of n_grad passes; 0 when
  * dims are invalid (see wm_validate) or n_grad < 1. */
 size_t wm_passes_backward_workspace(const wm_dims *dims, int32_t n_grad);
+
+/* ---- long contexts: a window of the cache, a shared prefix, eviction ------------------ */
+
+/* wm_channel_attend over a part of the cache: the row at position t, which wm_channel_attend
+ * lets read the slots below lim (lim = t in WM_MASK_PAPER, t + 1 in WM_MASK_INCLUSIVE), reads
+ * of them the last `window` ones and the first `sinks` ones: s < lim with s >= lim - window or
+ * s < sinks. The dummy slot of WM_MASK_PAPER stays visible. Single tokens (T_new <= 4), chunks
+ * and full sequences, contiguous tokens or one strided group. Slots that no row of the call
+ * reads are not used, whatever they hold; a NaN or infinity in a slot that some rows of a
+ * sequence read may reach that sequence's other rows.
+ *   window  >= 1; values past S_cap act as S_cap
+ *   sinks   >= 0
+ * Workspace: wm_workspace_size(dims, WM_OP_WINDOW_ATTEND). Other arguments and errors as
+ * wm_channel_attend, and WM_ERR_ARG for window < 1 or sinks < 0. */
+int wm_channel_attend_window(const wm_dims *dims, const wm_params *params, const void *Q,
+                             const int32_t *chan_map, const int32_t *ctx_len, int32_t window,
+                             int32_t sinks, const void *Kc, const void *Vc, void *O, void *ws,
+                             size_t ws_bytes, wm_stream_t stream);
+
+/* Gradients of wm_channel_attend_window for the output gradient dO, with P, dS and D = dO.O as
+ * in wm_channel_attend_backward over the slots each row reads. bf16 tensors, head dims 64 and
+ * 96, any T_new >= 1, contiguous tokens or one strided group. The weights and dS enter the
+ * products with 24 bits (three bf16 parts), the sums are fp32: the gradients are fp32 values of
+ * the formulas at the given O. Arguments, the slots of dKc and dVc that are written, and errors
+ * as wm_channel_attend_backward (without its limit on T_new); window and sinks as above.
+ * Workspace: wm_workspace_size(dims, WM_OP_WINDOW_BACKWARD). */
+int wm_channel_attend_window_backward(const wm_dims *dims, const wm_params *params,
+                                      const void *Q, const int32_t *chan_map,
+                                      const int32_t *ctx_len, int32_t window, int32_t sinks,
+                                      const void *Kc, const void *Vc, const void *O,
+                                      const void *dO, float *dQ, float *dKc, float *dVc,
+                                      float *dKd, float *dVd, void *ws, size_t ws_bytes,
+                                      wm_stream_t stream);
+
+/* Lays out the first prefix_len slots of one sequence as a prefix for
+ * wm_channel_attend_shared: Kp, Vp receive slots [0, prefix_len) of sequence seq of every
+ * channel and KV head, the keys turned back by prefix_len positions (RoPE is relative), so that
+ * the sequences that share the prefix count their own positions and cache slots from 0 and
+ * wm_q_project, wm_pool and wm_layer_attend need no offset. Keys are rounded to dtype once.
+ *   dims        B, k, Hkv, d, S_cap, dtype, rope_theta of the cache (T_new is not used)
+ *   Kc, Vc      device [k][B][Hkv][S_cap][d] in dtype
+ *   seq         0 <= seq < B
+ *   prefix_len  1 <= prefix_len <= min(S_cap, P_cap)
+ *   Kp, Vp      device [k][Hkv][P_cap][d] in dtype, apart from Kc and Vc; slots at and past
+ *               prefix_len are left as they are */
+int wm_prefix_share(const wm_dims *dims, const void *Kc, const void *Vc, int32_t seq,
+                    int32_t prefix_len, int32_t P_cap, void *Kp, void *Vp, wm_stream_t stream);
+
+/* wm_channel_attend for a batch whose sequences share a prefix: every row reads the
+ * prefix_len slots of its channel and KV head in Kp, Vp and, of its own sequence's cache, the
+ * slots wm_channel_attend lets it read; one softmax over both and the dummy slot. ctx_len and
+ * the positions count the sequence's own tokens, from 0 after the prefix.
+ *   prefix_len  0 <= prefix_len <= P_cap (0: Kp and Vp are not read and may be NULL)
+ *   Kp, Vp      device [k][Hkv][P_cap][d] in dtype (see wm_prefix_share)
+ * Few new tokens (T_new <= 4): the prefix is read once for the whole batch. Other arguments
+ * and errors as wm_channel_attend; workspace: wm_shared_workspace(dims, prefix_len). */
+int wm_channel_attend_shared(const wm_dims *dims, const wm_params *params, const void *Q,
+                             const int32_t *chan_map, const int32_t *ctx_len,
+                             int32_t prefix_len, int32_t P_cap, const void *Kp, const void *Vp,
+                             const void *Kc, const void *Vc, void *O, void *ws, size_t ws_bytes,
+                             wm_stream_t stream);
+/* Bytes of workspace wm_channel_attend_shared needs; 0 when dims are invalid or
+ * prefix_len < 0. */
+size_t wm_shared_workspace(const wm_dims *dims, int32_t prefix_len);
+
+/* wm_channel_attend that also adds up the softmax weight each cached slot receives, the score
+ * by which wm_cache_evict chooses:
+ *   weight  device float [k][B][Hkv][S_cap]: weight[c][b][h][s] += the sum of P over the rows
+ *           that read the slot (every consumer of the channel, every query head of the KV head,
+ *           every new token). Slots no row reads are left as they are; the dummy's weight is
+ *           not kept.
+ * Workspace: wm_workspace_size(dims, WM_OP_WEIGH_ATTEND). Other arguments and errors as
+ * wm_channel_attend. */
+int wm_channel_attend_weigh(const wm_dims *dims, const wm_params *params, const void *Q,
+                            const int32_t *chan_map, const int32_t *ctx_len, const void *Kc,
+                            const void *Vc, void *O, float *weight, void *ws, size_t ws_bytes,
+                            wm_stream_t stream);
+
+/* Cuts every sequence's cache to at most `keep` slots per (channel, KV head) and moves them to
+ * another cache. A sequence with n = ctx_len[b] > keep slots keeps the first `first`, the last
+ * `recent` and, of the rest, the keep - first - recent with the largest weight (equal weights:
+ * the lower slot; NaN counts as the smallest), in slot order; shorter sequences keep all. The
+ * j-th kept slot, from slot s, becomes slot j: its key turned by j - s positions (so that slot =
+ * position holds again and every other call continues from ctx_out), rounded to dtype once;
+ * its value and weight as they are.
+ *   dims        B, k, Hkv, d, S_cap, ctx_max, dtype, rope_theta (T_new is not used)
+ *   ctx_len     device int32 [B] in [0, ctx_max] or NULL (empty sequences)
+ *   keep        >= 1, first >= 0, recent >= 0, first + recent <= keep
+ *   weight      device float [k][B][Hkv][S_cap] (see wm_channel_attend_weigh)
+ *   S_out       slots per (channel, sequence, KV head) of the new cache, >= keep
+ *   ctx_out     device int32 [B]: min(ctx_len[b], keep)
+ *   weight_out  device float [k][B][Hkv][S_out]: the kept weights, zero from ctx_out[b] on
+ *   Ko, Vo      device [k][B][Hkv][S_out][d] in dtype; slots from ctx_out[b] on are left as
+ *               they are
+ *   kept        device int32 [k][B][Hkv][keep] or NULL: each kept slot's s, -1 from ctx_out[b]
+ *               on
+ * No output may overlap an input. Workspace: wm_workspace_size(dims, WM_OP_CACHE_EVICT). */
+int wm_cache_evict(const wm_dims *dims, const int32_t *ctx_len, int32_t keep, int32_t first,
+                   int32_t recent, const float *weight, const void *Kc, const void *Vc,
+                   int32_t S_out, int32_t *ctx_out, float *weight_out, void *Ko, void *Vo,
+                   int32_t *kept, void *ws, size_t ws_bytes, wm_stream_t stream);
 
 /* Measurement helper: wm_layer_step (doc_start NULL) or wm_layer_step_doc
  * (doc_start not NULL) that also records caller-created HIP events (hipEvent_t,

@@ -25,7 +25,9 @@ MASK_PAPER, MASK_INCLUSIVE = 0, 1
 ROUTER_DYNAMIC, ROUTER_STATIC, ROUTER_NOFEEDBACK = 0, 1, 2
 (OP_ROUTER_MIX, OP_KV_PROJECT, OP_Q_PROJECT, OP_CHANNEL_ATTEND, OP_LAYER_STEP, OP_POOL,
  OP_LAYER_ATTEND, OP_PASSES, OP_DENSE_ATTEND, OP_ATTEND_BACKWARD, OP_Q_BACKWARD,
- OP_POOL_BACKWARD, OP_STEP_BACKWARD, OP_PASSES_BACKWARD) = range(14)
+ OP_POOL_BACKWARD, OP_STEP_BACKWARD, OP_PASSES_BACKWARD, OP_WINDOW_ATTEND,
+ OP_WINDOW_BACKWARD, OP_SHARED_ATTEND, OP_WEIGH_ATTEND, OP_CACHE_EVICT,
+ OP_PREFIX_SHARE) = range(20)
 
 PARAM_NAMES = ("g_pre", "W_alpha", "b_alpha", "g_mid", "Wk", "Wv", "g_knorm",
                "Kd", "Vd", "g_in", "Wq", "g_qnorm")
@@ -60,6 +62,7 @@ class Grads(ctypes.Structure):
 
 _lib = None
 _vp, _i32p, _sz = ctypes.c_void_p, ctypes.POINTER(ctypes.c_int32), ctypes.c_size_t
+_i32 = ctypes.c_int32
 
 
 def lib() -> ctypes.CDLL:
@@ -96,6 +99,16 @@ def lib() -> ctypes.CDLL:
         "wm_layer_attend": [D, P, ctypes.c_int32, _vp, _i32p, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
         "wm_prefill_passes": [D, P, _vp, _vp, _i32p, ctypes.c_int32, _vp, _vp, _vp, _vp, _vp,
                               _sz, _vp],
+        "wm_channel_attend_window": [D, P, _vp, _i32p, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _sz,
+                                     _vp],
+        "wm_channel_attend_window_backward": [D, P, _vp, _i32p, _vp, _i32, _i32, _vp, _vp, _vp,
+                                              _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
+        "wm_prefix_share": [D, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp],
+        "wm_channel_attend_shared": [D, P, _vp, _i32p, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                                     _vp, _sz, _vp],
+        "wm_channel_attend_weigh": [D, P, _vp, _i32p, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
+        "wm_cache_evict": [D, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp,
+                           _vp, _vp, _sz, _vp],
         "wm_validate": [D, ctypes.c_int, _i32p],
         "wm_channel_groups": [ctypes.c_int32, ctypes.c_int32, _i32p, _i32p, _i32p],
         "wm_default_map": [ctypes.c_int32, ctypes.c_int32, _i32p],
@@ -111,6 +124,8 @@ def lib() -> ctypes.CDLL:
     L.wm_workspace_size.restype = ctypes.c_size_t
     L.wm_passes_backward_workspace.argtypes = [D, ctypes.c_int32]
     L.wm_passes_backward_workspace.restype = ctypes.c_size_t
+    L.wm_shared_workspace.argtypes = [D, ctypes.c_int32]
+    L.wm_shared_workspace.restype = ctypes.c_size_t
     L.wm_last_error.restype = ctypes.c_char_p
     L.wm_version.restype = ctypes.c_char_p
     _lib = L
@@ -391,6 +406,124 @@ def prefill_passes(dims: Dims, params, W_o, X, chan_map, passes: int, Kc, Vc, H,
     _check(lib().wm_prefill_passes(ctypes.byref(dims), _pref(params), _ptr(W_o), _ptr(X),
                                    _map(chan_map), int(passes), _ptr(Kc), _ptr(Vc), _ptr(H),
                                    _ptr(h_top), wp, wn, _stream(stream)))
+
+
+# ------------------------------------------------------------ long contexts
+
+def _want(name, t, shape, dtype):
+    """The tensor's pointer, once its shape and type are what the call reads or writes."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError("%s must be %s of shape %s, got %s of shape %s" %
+                         (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    return _ptr(t)
+
+
+def _elem(dims):
+    return torch.bfloat16 if dims.dtype == BF16 else torch.float32
+
+
+def _cache_ptrs(dims, **caches):
+    shape = (dims.k, dims.B, dims.Hkv, dims.S_cap, dims.d)
+    return [_want(n, t, shape, _elem(dims)) for n, t in caches.items()]
+
+
+def _attend_ptrs(dims, Q, ctx_len, Kc, Vc, O):
+    return (_want("Q", Q, (dims.L, dims.B, dims.Hq, dims.T_new, dims.d), _elem(dims)),
+            _want("ctx_len", ctx_len, (dims.B,), torch.int32),
+            *_cache_ptrs(dims, Kc=Kc, Vc=Vc),
+            _want("O", O, (dims.L, dims.B, dims.T_new, dims.Hq * dims.d), _elem(dims)))
+
+
+def channel_attend_window(dims: Dims, params, Q, chan_map, ctx_len, window: int, sinks: int, Kc,
+                          Vc, O, ws=None, stream=None):
+    """channel_attend over the last `window` slots each row may read and the first `sinks`."""
+    q, ctx, kc, vc, o = _attend_ptrs(dims, Q, ctx_len, Kc, Vc, O)
+    ws, wp, wn = _ws(dims, OP_WINDOW_ATTEND, ws, getattr(Q, "device", None))
+    _check(lib().wm_channel_attend_window(ctypes.byref(dims), _pref(params), q, _map(chan_map),
+                                          ctx, window, sinks, kc, vc, o, wp, wn,
+                                          _stream(stream)))
+
+
+def channel_attend_window_backward(dims: Dims, params, Q, chan_map, ctx_len, window: int,
+                                   sinks: int, Kc, Vc, O, dO, dQ, dKc, dVc, dKd, dVd, ws=None,
+                                   stream=None):
+    """Gradients of channel_attend_window for the output gradient dO: dQ, dKc, dVc, dKd, dVd
+    (device float32 tensors, written)."""
+    q, ctx, kc, vc, o = _attend_ptrs(dims, Q, ctx_len, Kc, Vc, O)
+    f32, dummy = torch.float32, (dims.k, dims.Hkv, dims.d)
+    out = [_want("dO", dO, (dims.L, dims.B, dims.T_new, dims.Hq * dims.d), _elem(dims)),
+           _want("dQ", dQ, (dims.L, dims.B, dims.Hq, dims.T_new, dims.d), f32),
+           *(_want(n, t, (dims.k, dims.B, dims.Hkv, dims.S_cap, dims.d), f32)
+             for n, t in (("dKc", dKc), ("dVc", dVc))),
+           _want("dKd", dKd, dummy, f32), _want("dVd", dVd, dummy, f32)]
+    ws, wp, wn = _ws(dims, OP_WINDOW_BACKWARD, ws, getattr(Q, "device", None))
+    _check(lib().wm_channel_attend_window_backward(ctypes.byref(dims), _pref(params), q,
+                                                   _map(chan_map), ctx, window, sinks, kc, vc, o,
+                                                   *out, wp, wn, _stream(stream)))
+
+
+def prefix_share(dims: Dims, Kc, Vc, seq: int, prefix_len: int, Kp, Vp, stream=None):
+    """Slots [0, prefix_len) of sequence seq into Kp, Vp [k, Hkv, P_cap, d], the keys turned
+    back by prefix_len positions: the prefix that channel_attend_shared reads."""
+    kc, vc = _cache_ptrs(dims, Kc=Kc, Vc=Vc)
+    P_cap = Kp.shape[2] if Kp is not None and Kp.dim() == 4 else 0
+    kp, vp = (_want(n, t, (dims.k, dims.Hkv, P_cap, dims.d), _elem(dims))
+              for n, t in (("Kp", Kp), ("Vp", Vp)))
+    _check(lib().wm_prefix_share(ctypes.byref(dims), kc, vc, seq, prefix_len, P_cap, kp, vp,
+                                 _stream(stream)))
+
+
+def shared_workspace(dims: Dims, prefix_len: int) -> int:
+    return int(lib().wm_shared_workspace(ctypes.byref(dims), prefix_len))
+
+
+def channel_attend_shared(dims: Dims, params, Q, chan_map, ctx_len, prefix_len: int, Kp, Vp, Kc,
+                          Vc, O, ws=None, stream=None):
+    """channel_attend of rows that also read the batch's prefix Kp, Vp [k, Hkv, P_cap, d]."""
+    q, ctx, kc, vc, o = _attend_ptrs(dims, Q, ctx_len, Kc, Vc, O)
+    P_cap = Kp.shape[2] if Kp is not None and Kp.dim() == 4 else 0
+    kp, vp = (_want(n, t, (dims.k, dims.Hkv, P_cap, dims.d), _elem(dims))
+              for n, t in (("Kp", Kp), ("Vp", Vp)))
+    if ws is None and getattr(Q, "device", None) is not None:
+        ws = torch.empty(max(shared_workspace(dims, prefix_len), 256), dtype=torch.uint8,
+                         device=Q.device)
+    wp, wn = (ws.data_ptr(), ws.numel()) if ws is not None else (None, 0)
+    _check(lib().wm_channel_attend_shared(ctypes.byref(dims), _pref(params), q, _map(chan_map),
+                                          ctx, prefix_len, P_cap, kp, vp, kc, vc, o, wp, wn,
+                                          _stream(stream)))
+
+
+def channel_attend_weigh(dims: Dims, params, Q, chan_map, ctx_len, Kc, Vc, O, weight, ws=None,
+                         stream=None):
+    """channel_attend that adds each slot's received softmax weight to weight (device float32
+    [k, B, Hkv, S_cap])."""
+    q, ctx, kc, vc, o = _attend_ptrs(dims, Q, ctx_len, Kc, Vc, O)
+    w = _want("weight", weight, (dims.k, dims.B, dims.Hkv, dims.S_cap), torch.float32)
+    ws, wp, wn = _ws(dims, OP_WEIGH_ATTEND, ws, getattr(Q, "device", None))
+    _check(lib().wm_channel_attend_weigh(ctypes.byref(dims), _pref(params), q, _map(chan_map),
+                                         ctx, kc, vc, o, w, wp, wn, _stream(stream)))
+
+
+def cache_evict(dims: Dims, ctx_len, keep: int, first: int, recent: int, weight, Kc, Vc, ctx_out,
+                weight_out, Ko, Vo, kept=None, ws=None, stream=None):
+    """At most keep slots of every (channel, sequence, KV head) moved to the cache Ko, Vo
+    [k, B, Hkv, S_out, d]: the first, the recent and the heaviest others, in order, keys turned
+    to their new positions; ctx_out, weight_out and (optional) kept go with them."""
+    kc, vc = _cache_ptrs(dims, Kc=Kc, Vc=Vc)
+    slices = (dims.k, dims.B, dims.Hkv)
+    S_out = Ko.shape[3] if Ko is not None and Ko.dim() == 5 else 0
+    w = _want("weight", weight, (*slices, dims.S_cap), torch.float32)
+    ctx = _want("ctx_len", ctx_len, (dims.B,), torch.int32)
+    co = _want("ctx_out", ctx_out, (dims.B,), torch.int32)
+    wo = _want("weight_out", weight_out, (*slices, S_out), torch.float32)
+    ko, vo = (_want(n, t, (*slices, S_out, dims.d), _elem(dims))
+              for n, t in (("Ko", Ko), ("Vo", Vo)))
+    kd = _want("kept", kept, (*slices, keep), torch.int32)
+    ws, wp, wn = _ws(dims, OP_CACHE_EVICT, ws, getattr(Kc, "device", None))
+    _check(lib().wm_cache_evict(ctypes.byref(dims), ctx, keep, first, recent, w, kc, vc, S_out,
+                                co, wo, ko, vo, kd, wp, wn, _stream(stream)))
 
 
 PROFILE_EVENTS = 7

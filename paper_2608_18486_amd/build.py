@@ -24,6 +24,8 @@ SOURCES = {
     "wm_few.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "wm_backward.hip": [],
     "wm_grad.hip": [],
+    "wm_reach.hip": [],
+    "wm_evict.hip": [],
     "wm_calib.hip": [],
 }
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -48,6 +48,7 @@ struct Layout {
   // K/V pre-norm values and gradients, channel gradients, state gradients, logit gradients
   size_t dq = 0, dgp = 0, gkd = 0, x = 0, yq = 0, dyq = 0, dx = 0, hn = 0, u = 0, ydy = 0,
          dyb = 0, du = 0, dhn = 0, dlog = 0, dlogb = 0, split = 0;
+  size_t lse = 0;  // weighed attention: log-sum-exp per row
 };
 
 int group_stride(const wm_dims& d) { return d.groups > 1 ? d.groups : 1; }
@@ -239,6 +240,12 @@ Layout layout(const wm_dims& dd, int op) {
     if (decode_path(d)) Ly.part = take(wm::decode_partials_bytes(dense_shape(make_shape(d))));
   }
   if (layer && decode_path(d)) Ly.part = take(wm::decode_partials_bytes(one_layer(make_shape(d))));
+  if (op == WM_OP_WINDOW_BACKWARD) Ly.part = take(wm::reach_backward_rows_bytes(make_shape(d)));
+  if (op == WM_OP_WEIGH_ATTEND) Ly.lse = take((size_t)d.L * N * d.Hq * 4);
+  if (op == WM_OP_CACHE_EVICT) {
+    Ly.total = d.B == 0 ? 0 : al256(wm::evict_index_bytes(make_shape(d)));
+    return Ly;
+  }
   if (op == WM_OP_ATTEND_BACKWARD) Ly.part = take(wm::attend_backward_rows_bytes(make_shape(d)));
   // the full-sequence attention's work queue (or its split ranges' partial states) takes
   // the decode partials' place
@@ -262,13 +269,14 @@ bool uses_cache(int op) {
   return op == WM_OP_KV_PROJECT || op == WM_OP_CHANNEL_ATTEND || op == WM_OP_LAYER_STEP ||
          op == WM_OP_POOL || op == WM_OP_LAYER_ATTEND || op == WM_OP_PASSES ||
          op == WM_OP_DENSE_ATTEND || op == WM_OP_ATTEND_BACKWARD || op == WM_OP_POOL_BACKWARD ||
-         op == WM_OP_STEP_BACKWARD || op == WM_OP_PASSES_BACKWARD;
+         op == WM_OP_STEP_BACKWARD || op == WM_OP_PASSES_BACKWARD ||
+         (op >= WM_OP_WINDOW_ATTEND && op <= WM_OP_PREFIX_SHARE);
 }
 
 int validate_dims(const wm_dims* dp, int op, const int32_t* chan_map) {
   if (!dp) return fail(WM_ERR_ARG, "dims is NULL");
   const wm_dims& d = *dp;
-  if (op < WM_OP_ROUTER_MIX || op > WM_OP_PASSES_BACKWARD) return fail(WM_ERR_ARG, "unknown op %d", op);
+  if (op < WM_OP_ROUTER_MIX || op > WM_OP_PREFIX_SHARE) return fail(WM_ERR_ARG, "unknown op %d", op);
   if (d.dtype != WM_F32 && d.dtype != WM_BF16) return fail(WM_ERR_DTYPE, "unknown dtype %d", d.dtype);
   if (d.mix_mode != WM_MIX_LINEAR && d.mix_mode != WM_MIX_SOFTMAX)
     return fail(WM_ERR_DTYPE, "unknown mix_mode %d", d.mix_mode);
@@ -353,13 +361,16 @@ int need_ptr(const void* p, const char* name) {
   return WM_OK;
 }
 
-int check_ws(const wm_dims& d, int op, void* ws, size_t ws_bytes) {
-  size_t need = layout(d, op).total;
+int check_ws_bytes(size_t need, void* ws, size_t ws_bytes) {
   if (need == 0) return WM_OK;
   if (!ws) return fail(WM_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
   if ((uintptr_t)ws % 256 != 0) return fail(WM_ERR_WORKSPACE, "workspace is not 256-byte aligned");
   if (ws_bytes < need) return fail(WM_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
   return WM_OK;
+}
+
+int check_ws(const wm_dims& d, int op, void* ws, size_t ws_bytes) {
+  return check_ws_bytes(layout(d, op).total, ws, ws_bytes);
 }
 
 int launched() {
@@ -722,7 +733,6 @@ int static_scratch(void** out) {
   return WM_OK;
 }
 
-
 // ------------------------------------------------------------------ gradients
 wm::GemmOperand opnd(const void* p, long s_row, long s_k, long s_z, bool f32, bool pad8 = false) {
   return wm::GemmOperand{p, s_row, s_k, s_z, f32 ? 1 : 0, pad8 ? 1 : 0, 0};
@@ -906,7 +916,6 @@ void run_pool_backward(const wm_dims& d, const wm_params& P, const bf16* H,
     wm::launch_grad_sum(dgp, L, nch, D, G.g_pre + (long)br * L * D, 1.f, 1, s);
   }
 }
-
 
 // ------------------------------------------- Section 3.3: truncated backpropagation
 // Workspace of wm_prefill_passes_backward: the forward's scratch, what the gradient
@@ -1136,6 +1145,65 @@ void run_passes_backward(const wm_dims& d, const wm_params& P, const bf16* W_o, 
       wm::launch_grad_add_rows(dX + (long)q * D, (long)g * D, dhn, Ng, D, (long)L * D, L, s);
     }
   }
+}
+
+// ------------------------------------------------------------------ long contexts
+// Window, prefix and weight calls share their checks with wm_channel_attend.
+int check_attend(const wm_dims* dims, int op, const wm_params* params, const void* Q,
+                        const int32_t* chan_map, const void* Kc, const void* Vc, const void* O) {
+  if (!chan_map) return fail(WM_ERR_ARG, "chan_map is NULL");
+  WM_TRY(validate_dims(dims, op, chan_map));
+  if ((size_t)dims->B * dims->T_new == 0) return WM_OK;
+  if (dims->mask_mode == WM_MASK_PAPER) WM_TRY(check_params(params, {P_KD, P_VD}));
+  else if (!params) return fail(WM_ERR_ARG, "params is NULL");
+  WM_TRY(need_ptr(Q, "Q"));
+  WM_TRY(need_ptr(Kc, "Kc"));
+  WM_TRY(need_ptr(Vc, "Vc"));
+  return need_ptr(O, "O");
+}
+
+int check_window(int32_t window, int32_t sinks) {
+  if (window < 1) return fail(WM_ERR_ARG, "window must be >= 1");
+  if (sinks < 0) return fail(WM_ERR_ARG, "sinks must be >= 0");
+  return WM_OK;
+}
+
+wm::Reach window_reach(const wm_dims& d, int32_t window, int32_t sinks) {
+  return wm::Reach{nullptr, nullptr, 0, 0, std::min(window, d.S_cap), std::min(sinks, d.S_cap)};
+}
+
+bool overlap(const void* p, size_t n, const void* q, size_t m) {
+  return (uintptr_t)p < (uintptr_t)q + m && (uintptr_t)q < (uintptr_t)p + n;
+}
+
+int check_prefix(const wm_dims& d, int32_t prefix_len, int32_t P_cap) {
+  if (prefix_len < 0) return fail(WM_ERR_ARG, "prefix_len must be >= 0");
+  if (prefix_len > P_cap)
+    return fail(WM_ERR_CAPACITY, "prefix_len = %d exceeds P_cap = %d", prefix_len, P_cap);
+  if ((double)P_cap * d.d * elem_size(d) >= 2147483647.0)
+    return fail(WM_ERR_SHAPE, "a slice of the prefix spans more than 2 GiB");
+  if ((long long)prefix_len + d.ctx_max + call_span(d) > INT_MAX / 2)
+    return fail(WM_ERR_SHAPE, "positions past the 32-bit range");
+  return WM_OK;
+}
+
+size_t shared_ws(const wm_dims& d, int32_t prefix_len) {
+  (void)d;
+  (void)prefix_len;
+  return 0;
+}
+
+template <typename T>
+void run_weigh(const wm_dims& d, const wm_params& P, const T* Q, const int32_t* chan_map,
+                      const int32_t* ctx_len, const T* Kc, const T* Vc, T* O, float* weight,
+                      void* ws, hipStream_t s) {
+  const wm::Shape sh = make_shape(d);
+  const wm::Reach r{nullptr, nullptr, 0, 0, d.S_cap, 0};
+  float* lse = (float*)at(ws, layout(d, WM_OP_WEIGH_ATTEND).lse);
+  wm::launch_reach<T>(sh, r, map_table(d, chan_map), Q, Kc, Vc, (const T*)P.Kd, (const T*)P.Vd,
+                      ctx_len, O, lse, s);
+  wm::launch_weigh<T>(sh, map_table(d, chan_map), groups(d, chan_map), Q, Kc, ctx_len, lse,
+                      weight, s);
 }
 
 }  // namespace
@@ -1693,6 +1761,190 @@ int wm_prefill_passes_backward(const wm_dims* dims, const wm_params* params, con
   (void)hipGetLastError();
   run_passes_backward(d, *params, (const bf16*)W_o, (const bf16*)X, chan_map, passes, n_grad,
                       dh_top, (bf16*)h_top, dX, dW_o, *grads, ws, (hipStream_t)stream);
+  return launched();
+}
+
+// ---- long contexts
+
+int wm_channel_attend_window(const wm_dims* dims, const wm_params* params, const void* Q,
+                             const int32_t* chan_map, const int32_t* ctx_len, int32_t window,
+                             int32_t sinks, const void* Kc, const void* Vc, void* O, void* ws,
+                             size_t ws_bytes, wm_stream_t stream) {
+  WM_TRY(check_window(window, sinks));
+  WM_TRY(check_attend(dims, WM_OP_WINDOW_ATTEND, params, Q, chan_map, Kc, Vc, O));
+  const wm_dims& d = *dims;
+  if ((size_t)d.B * d.T_new == 0) return WM_OK;
+  WM_TRY(check_ws(d, WM_OP_WINDOW_ATTEND, ws, ws_bytes));
+  (void)hipGetLastError();
+  const wm::Reach r = window_reach(d, window, sinks);
+  hipStream_t s = (hipStream_t)stream;
+  if (d.dtype == WM_BF16)
+    wm::launch_reach<bf16>(make_shape(d), r, map_table(d, chan_map), (const bf16*)Q,
+                           (const bf16*)Kc, (const bf16*)Vc, (const bf16*)params->Kd,
+                           (const bf16*)params->Vd, ctx_len, (bf16*)O, nullptr, s);
+  else
+    wm::launch_reach<float>(make_shape(d), r, map_table(d, chan_map), (const float*)Q,
+                            (const float*)Kc, (const float*)Vc, (const float*)params->Kd,
+                            (const float*)params->Vd, ctx_len, (float*)O, nullptr, s);
+  return launched();
+}
+
+int wm_channel_attend_window_backward(const wm_dims* dims, const wm_params* params, const void* Q,
+                                      const int32_t* chan_map, const int32_t* ctx_len,
+                                      int32_t window, int32_t sinks, const void* Kc,
+                                      const void* Vc, const void* O, const void* dO, float* dQ,
+                                      float* dKc, float* dVc, float* dKd, float* dVd, void* ws,
+                                      size_t ws_bytes, wm_stream_t stream) {
+  WM_TRY(check_window(window, sinks));
+  WM_TRY(check_attend(dims, WM_OP_WINDOW_BACKWARD, params, Q, chan_map, Kc, Vc, O));
+  const wm_dims& d = *dims;
+  if (d.dtype != WM_BF16) return fail(WM_ERR_DTYPE, "the attention gradients are built for bf16");
+  if (d.d != 64 && d.d != 96)
+    return fail(WM_ERR_SHAPE, "the attention gradients support head dims 64 and 96");
+  if ((size_t)d.B * d.T_new == 0) return WM_OK;
+  WM_TRY(need_ptr(dO, "dO"));
+  WM_TRY(need_ptr(dQ, "dQ"));
+  WM_TRY(need_ptr(dKc, "dKc"));
+  WM_TRY(need_ptr(dVc, "dVc"));
+  WM_TRY(need_ptr(dKd, "dKd"));
+  WM_TRY(need_ptr(dVd, "dVd"));
+  WM_TRY(check_ws(d, WM_OP_WINDOW_BACKWARD, ws, ws_bytes));
+  (void)hipGetLastError();
+  wm::launch_reach_backward(make_shape(d), window_reach(d, window, sinks), map_table(d, chan_map),
+                            groups(d, chan_map), (const bf16*)Q, (const bf16*)Kc,
+                            (const bf16*)Vc, (const bf16*)params->Kd, (const bf16*)params->Vd,
+                            (const bf16*)O, (const bf16*)dO, ctx_len, dQ, dKc, dVc, dKd, dVd,
+                            (float*)at(ws, layout(d, WM_OP_WINDOW_BACKWARD).part),
+                            (hipStream_t)stream);
+  return launched();
+}
+
+int wm_prefix_share(const wm_dims* dims, const void* Kc, const void* Vc, int32_t seq,
+                    int32_t prefix_len, int32_t P_cap, void* Kp, void* Vp, wm_stream_t stream) {
+  WM_TRY(validate_dims(dims, WM_OP_PREFIX_SHARE, nullptr));
+  const wm_dims& d = *dims;
+  if (seq < 0 || seq >= d.B) return fail(WM_ERR_ARG, "seq must be in [0, B)");
+  if (prefix_len < 1) return fail(WM_ERR_ARG, "prefix_len must be >= 1");
+  if (prefix_len > d.S_cap || prefix_len > P_cap)
+    return fail(WM_ERR_CAPACITY, "prefix_len = %d exceeds S_cap = %d or P_cap = %d", prefix_len,
+                d.S_cap, P_cap);
+  if ((double)P_cap * d.d * elem_size(d) >= 2147483647.0)
+    return fail(WM_ERR_SHAPE, "a slice of the prefix spans more than 2 GiB");
+  WM_TRY(need_ptr(Kc, "Kc"));
+  WM_TRY(need_ptr(Vc, "Vc"));
+  WM_TRY(need_ptr(Kp, "Kp"));
+  WM_TRY(need_ptr(Vp, "Vp"));
+  const size_t row = (size_t)d.k * d.Hkv * d.d * elem_size(d);
+  const size_t from = row * d.B * d.S_cap, to = row * P_cap;
+  if (overlap(Kp, to, Vp, to) || overlap(Kp, to, Kc, from) || overlap(Kp, to, Vc, from) ||
+      overlap(Vp, to, Kc, from) || overlap(Vp, to, Vc, from))
+    return fail(WM_ERR_ARG, "Kp and Vp must not overlap the cache or each other");
+  (void)hipGetLastError();
+  wm::launch_prefix_share(make_shape(d), Kc, Vc, seq, prefix_len, P_cap, Kp, Vp,
+                          d.dtype == WM_BF16, (hipStream_t)stream);
+  return launched();
+}
+
+size_t wm_shared_workspace(const wm_dims* dims, int32_t prefix_len) {
+  if (validate_dims(dims, WM_OP_SHARED_ATTEND, nullptr) != WM_OK) return 0;
+  if (check_prefix(*dims, prefix_len, prefix_len) != WM_OK) return 0;
+  return shared_ws(*dims, prefix_len);
+}
+
+int wm_channel_attend_shared(const wm_dims* dims, const wm_params* params, const void* Q,
+                             const int32_t* chan_map, const int32_t* ctx_len, int32_t prefix_len,
+                             int32_t P_cap, const void* Kp, const void* Vp, const void* Kc,
+                             const void* Vc, void* O, void* ws, size_t ws_bytes,
+                             wm_stream_t stream) {
+  WM_TRY(check_attend(dims, WM_OP_SHARED_ATTEND, params, Q, chan_map, Kc, Vc, O));
+  const wm_dims& d = *dims;
+  WM_TRY(check_prefix(d, prefix_len, P_cap));
+  if ((size_t)d.B * d.T_new == 0) return WM_OK;
+  if (prefix_len > 0) {
+    WM_TRY(need_ptr(Kp, "Kp"));
+    WM_TRY(need_ptr(Vp, "Vp"));
+  }
+  WM_TRY(check_ws_bytes(shared_ws(d, prefix_len), ws, ws_bytes));
+  (void)hipGetLastError();
+  const wm::Reach r{Kp, Vp, prefix_len, P_cap, d.S_cap, 0};
+  hipStream_t s = (hipStream_t)stream;
+  if (d.dtype == WM_BF16)
+    wm::launch_reach<bf16>(make_shape(d), r, map_table(d, chan_map), (const bf16*)Q,
+                           (const bf16*)Kc, (const bf16*)Vc, (const bf16*)params->Kd,
+                           (const bf16*)params->Vd, ctx_len, (bf16*)O, nullptr, s);
+  else
+    wm::launch_reach<float>(make_shape(d), r, map_table(d, chan_map), (const float*)Q,
+                            (const float*)Kc, (const float*)Vc, (const float*)params->Kd,
+                            (const float*)params->Vd, ctx_len, (float*)O, nullptr, s);
+  return launched();
+}
+
+int wm_channel_attend_weigh(const wm_dims* dims, const wm_params* params, const void* Q,
+                            const int32_t* chan_map, const int32_t* ctx_len, const void* Kc,
+                            const void* Vc, void* O, float* weight, void* ws, size_t ws_bytes,
+                            wm_stream_t stream) {
+  WM_TRY(check_attend(dims, WM_OP_WEIGH_ATTEND, params, Q, chan_map, Kc, Vc, O));
+  const wm_dims& d = *dims;
+  if ((size_t)d.B * d.T_new == 0) return WM_OK;
+  WM_TRY(need_ptr(weight, "weight"));
+  WM_TRY(check_ws(d, WM_OP_WEIGH_ATTEND, ws, ws_bytes));
+  (void)hipGetLastError();
+  hipStream_t s = (hipStream_t)stream;
+  if (d.dtype == WM_BF16)
+    run_weigh<bf16>(d, *params, (const bf16*)Q, chan_map, ctx_len, (const bf16*)Kc,
+                    (const bf16*)Vc, (bf16*)O, weight, ws, s);
+  else
+    run_weigh<float>(d, *params, (const float*)Q, chan_map, ctx_len, (const float*)Kc,
+                     (const float*)Vc, (float*)O, weight, ws, s);
+  return launched();
+}
+
+int wm_cache_evict(const wm_dims* dims, const int32_t* ctx_len, int32_t keep, int32_t first,
+                   int32_t recent, const float* weight, const void* Kc, const void* Vc,
+                   int32_t S_out, int32_t* ctx_out, float* weight_out, void* Ko, void* Vo,
+                   int32_t* kept, void* ws, size_t ws_bytes, wm_stream_t stream) {
+  WM_TRY(validate_dims(dims, WM_OP_CACHE_EVICT, nullptr));
+  const wm_dims& d = *dims;
+  if (keep < 1) return fail(WM_ERR_ARG, "keep must be >= 1");
+  if (first < 0 || recent < 0 || (long long)first + recent > keep)
+    return fail(WM_ERR_ARG, "first and recent must be >= 0 and at most keep together");
+  if (keep > S_out) return fail(WM_ERR_CAPACITY, "keep = %d exceeds S_out = %d", keep, S_out);
+  if ((double)S_out * d.d * elem_size(d) >= 2147483647.0)
+    return fail(WM_ERR_SHAPE, "a slice of the new cache spans more than 2 GiB");
+  if (d.B == 0) return WM_OK;
+  WM_TRY(need_ptr(weight, "weight"));
+  WM_TRY(need_ptr(Kc, "Kc"));
+  WM_TRY(need_ptr(Vc, "Vc"));
+  WM_TRY(need_ptr(weight_out, "weight_out"));
+  WM_TRY(need_ptr(Ko, "Ko"));
+  WM_TRY(need_ptr(Vo, "Vo"));
+  if (!ctx_out) return fail(WM_ERR_ARG, "ctx_out is NULL");
+  if ((uintptr_t)ctx_out % 4 != 0 || (uintptr_t)kept % 4 != 0)
+    return fail(WM_ERR_ARG, "ctx_out or kept is not 4-byte aligned");
+  WM_TRY(check_ws(d, WM_OP_CACHE_EVICT, ws, ws_bytes));
+  const size_t slices = (size_t)d.k * d.B * d.Hkv, row = slices * d.d * elem_size(d);
+  struct { const void* p; size_t n; } in[] = {{ctx_len, ctx_len ? 4 * (size_t)d.B : 0},
+                                              {weight, 4 * slices * d.S_cap},
+                                              {Kc, row * d.S_cap},
+                                              {Vc, row * d.S_cap}},
+      out[] = {{ctx_out, 4 * (size_t)d.B},
+               {weight_out, 4 * slices * S_out},
+               {Ko, row * S_out},
+               {Vo, row * S_out},
+               {kept, kept ? 4 * slices * keep : 0},
+               {ws, ws_bytes}};
+  for (int i = 0; i < 6; ++i) {
+    for (const auto& x : in)
+      if (overlap(out[i].p, out[i].n, x.p, x.n))
+        return fail(WM_ERR_ARG, "an output of wm_cache_evict overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n))
+        return fail(WM_ERR_ARG, "two outputs of wm_cache_evict overlap");
+  }
+  (void)hipGetLastError();
+  wm::launch_evict(make_shape(d), ctx_len, keep, first, recent, weight, Kc, Vc, S_out, ctx_out,
+                   weight_out, Ko, Vo, kept, (int32_t*)ws, d.dtype == WM_BF16,
+                   (hipStream_t)stream);
   return launched();
 }
 

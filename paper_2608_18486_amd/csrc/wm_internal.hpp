@@ -279,6 +279,38 @@ void launch_soft_read(const Shape& sh, const float* w, const T* Kc, const T* Vc,
                       const T* Vd, const int32_t* ctx_len, T* Kl, T* Vl, T* Kdl, T* Vdl,
                       hipStream_t s);
 
+// -- long contexts (wm_reach.hip, wm_evict.hip) ------------------------------------------
+// What a row reads besides the dummy: P slots of a prefix common to the batch (Kp, Vp
+// [k][Hkv][P_cap][d]) and, of the cache slots below its limit, the last `window` and the first
+// `sinks`.
+struct Reach {
+  const void *Kp, *Vp;
+  int P, P_cap, window, sinks;
+};
+// lse: per row [L][B][Hq][T_new], in log2 units, or null
+template <typename T>
+void launch_reach(const Shape& sh, const Reach& r, const LayerTable& chan, const T* Q, const T* Kc,
+                  const T* Vc, const T* Kd, const T* Vd, const int32_t* ctx_len, T* O, float* lse,
+                  hipStream_t s);
+// weight[k][B][Hkv][S_cap] += the rows' weights on each slot, from their lse
+template <typename T>
+void launch_weigh(const Shape& sh, const LayerTable& chan, const ChannelGroups& cg, const T* Q,
+                  const T* Kc, const int32_t* ctx_len, const float* lse, float* weight,
+                  hipStream_t s);
+size_t reach_backward_rows_bytes(const Shape& sh);
+void launch_reach_backward(const Shape& sh, const Reach& r, const LayerTable& chan,
+                           const ChannelGroups& cg, const bf16* Q, const bf16* Kc, const bf16* Vc,
+                           const bf16* Kd, const bf16* Vd, const bf16* O, const bf16* dO,
+                           const int32_t* ctx_len, float* dQ, float* dKc, float* dVc, float* dKd,
+                           float* dVd, float* rows, hipStream_t s);
+size_t evict_index_bytes(const Shape& sh);
+void launch_evict(const Shape& sh, const int32_t* ctx_len, int keep, int first, int recent,
+                  const float* weight, const void* Kc, const void* Vc, int S_out,
+                  int32_t* ctx_out, float* weight_out, void* Ko, void* Vo, int32_t* kept,
+                  int32_t* idx, bool bf, hipStream_t s);
+void launch_prefix_share(const Shape& sh, const void* Kc, const void* Vc, int seq, int len,
+                         int P_cap, void* Kp, void* Vp, bool bf, hipStream_t s);
+
 // -- measurement helper ---------------------------------------------------------
 // blocks x 4 waves, each issuing 8 * iters independent 32x32x16 bf16 MFMAs on small
 // constant operands, or (random) on hashed operands that change from one MFMA to the next.
