@@ -240,6 +240,8 @@ Layout layout(const wm_dims& dd, int op) {
     if (decode_path(d)) Ly.part = take(wm::decode_partials_bytes(dense_shape(make_shape(d))));
   }
   if (layer && decode_path(d)) Ly.part = take(wm::decode_partials_bytes(one_layer(make_shape(d))));
+  if (op == WM_OP_WINDOW_ATTEND && decode_path(d))
+    Ly.part = take(wm::decode_window_bytes(make_shape(d)));
   if (op == WM_OP_WINDOW_BACKWARD) Ly.part = take(wm::reach_backward_rows_bytes(make_shape(d)));
   if (op == WM_OP_WEIGH_ATTEND) Ly.lse = take((size_t)d.L * N * d.Hq * 4);
   if (op == WM_OP_CACHE_EVICT) {
@@ -1172,6 +1174,21 @@ wm::Reach window_reach(const wm_dims& d, int32_t window, int32_t sinks) {
   return wm::Reach{nullptr, nullptr, 0, 0, std::min(window, d.S_cap), std::min(sinks, d.S_cap)};
 }
 
+template <typename T>
+void run_window(const wm_dims& d, const wm_params& P, const wm::Reach& r, const T* Q,
+                const int32_t* chan_map, const int32_t* ctx_len, const T* Kc, const T* Vc, T* O,
+                void* ws, hipStream_t s) {
+  const wm::Shape sh = make_shape(d);
+  const wm::LayerTable mt = map_table(d, chan_map);
+  if (decode_path(d))
+    wm::launch_attend_decode<T>(sh, mt, groups(d, chan_map), Q, Kc, Vc, (const T*)P.Kd,
+                                (const T*)P.Vd, ctx_len, nullptr,
+                                (float*)at(ws, layout(d, WM_OP_WINDOW_ATTEND).part), O, s, &r);
+  else
+    wm::launch_reach<T>(sh, r, mt, Q, Kc, Vc, (const T*)P.Kd, (const T*)P.Vd, ctx_len, O, nullptr,
+                        s);
+}
+
 bool overlap(const void* p, size_t n, const void* q, size_t m) {
   return (uintptr_t)p < (uintptr_t)q + m && (uintptr_t)q < (uintptr_t)p + n;
 }
@@ -1779,13 +1796,11 @@ int wm_channel_attend_window(const wm_dims* dims, const wm_params* params, const
   const wm::Reach r = window_reach(d, window, sinks);
   hipStream_t s = (hipStream_t)stream;
   if (d.dtype == WM_BF16)
-    wm::launch_reach<bf16>(make_shape(d), r, map_table(d, chan_map), (const bf16*)Q,
-                           (const bf16*)Kc, (const bf16*)Vc, (const bf16*)params->Kd,
-                           (const bf16*)params->Vd, ctx_len, (bf16*)O, nullptr, s);
+    run_window<bf16>(d, *params, r, (const bf16*)Q, chan_map, ctx_len, (const bf16*)Kc,
+                     (const bf16*)Vc, (bf16*)O, ws, s);
   else
-    wm::launch_reach<float>(make_shape(d), r, map_table(d, chan_map), (const float*)Q,
-                            (const float*)Kc, (const float*)Vc, (const float*)params->Kd,
-                            (const float*)params->Vd, ctx_len, (float*)O, nullptr, s);
+    run_window<float>(d, *params, r, (const float*)Q, chan_map, ctx_len, (const float*)Kc,
+                      (const float*)Vc, (float*)O, ws, s);
   return launched();
 }
 

@@ -39,6 +39,23 @@ size_t decode_partials_bytes(const Shape& sh) {
   return rows * decode_splits(sh) * (sh.d + 2) * sizeof(float);
 }
 
+// Slots that a sequence's rows read in all, at most (T_new rows whose windows move on by gs).
+long window_slots(const Shape& sh, const Reach& r) {
+  return std::min((long)sh.ctx_max + sh.span(),
+                  (long)r.sinks + r.window + (long)sh.gs * (sh.T_new - 1));
+}
+
+// The partials of a window call of these dims, whatever its window: decode_splits of a walk of
+// w slots is ceil(w / 256) until the grid holds kDecodeMinBlocks workgroups, then less than twice
+// what that takes, and from there on ceil(w / 4096).
+size_t decode_window_bytes(const Shape& sh) {
+  const long kend = (long)sh.ctx_max + sh.span(), slices = (long)sh.k * sh.B * sh.Hkv;
+  const long some = std::min((kend + kSplitMin - 1) / kSplitMin,
+                             std::max(1L, 2 * kDecodeMinBlocks / slices));
+  const long n = std::max(std::max(1L, (kend + kSplitMax - 1) / kSplitMax), some);
+  return (size_t)sh.L * sh.B * sh.Hq * sh.T_new * n * (sh.d + 2) * sizeof(float);
+}
+
 template <typename T> struct DecodeArgs {
   const T *Q, *Kc, *Vc, *Kd, *Vd;
   const int32_t* ctx_len;
@@ -52,7 +69,26 @@ template <typename T> struct DecodeArgs {
   // the grid's channels, those with a reader: live[i], its consumers offsets[i] .. offsets[i + 1]
   LayerTable live;
   ChannelGroups cg;
+  int window, sinks;  // WIN kernels: a row reads its last `window` slots and the first `sinks`
 };
+
+// The slots that a sequence's rows read in a window, one after the other: `na` first slots, then
+// those from lo0 (the first row's window, which starts lowest) on. Compact slot x is slot
+// x < na ? x : x + skip of the cache; a row with limit lim reads compact slots below lim - skip
+// that are at or past its lo - skip or below `sinks`. (skip > 0 only where every first slot lies
+// before every row's window, so that all rows read all of them; else compact = cache slots.)
+struct WindowSpan {
+  int na, skip, n, lo_last;  // n compact slots; lo_last: the last row's window's first one
+};
+__device__ __forceinline__ WindowSpan window_span(int lim0, int kend, int window, int sinks) {
+  WindowSpan w;
+  const int lo0 = max(lim0 - window, 0);
+  w.na = min(sinks, lo0);
+  w.skip = lo0 - w.na;
+  w.n = max(kend - w.skip, 0);
+  w.lo_last = max(kend - window, 0) - w.skip;
+  return w;
+}
 
 // Merge online-softmax state (m2, l2, o2) into (m, l, o).
 __device__ __forceinline__ void merge_state(float& m, float& l, float* o, float m2, float l2,
@@ -115,7 +151,7 @@ __device__ __forceinline__ void lds_dma16_stream(uint32_t lds_addr, uint32_t vof
                : "memory", "m0");
 }
 
-template <int DH, int NW, bool DOC, bool ONCE>
+template <int DH, int NW, bool DOC, bool ONCE, bool WIN = false>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(3)))
 void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
   using C = DecMfma<DH, NW>;
@@ -132,7 +168,10 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
   const int pos0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq;
   const int gs = a.gs, incl = a.mask_paper ? 0 : 1;
   const int kend = min(pos0 + gs * (a.T_new - 1) + incl, a.S_cap);
-  const int s0 = split * a.split_len, s1 = min(s0 + a.split_len, kend);
+  // (WIN: s0, s1 and every slot index below are compact)
+  WindowSpan ws{0, 0, 0, 0};
+  if constexpr (WIN) ws = window_span(pos0 + incl, kend, a.window, a.sinks);
+  const int s0 = split * a.split_len, s1 = min(s0 + a.split_len, WIN ? ws.n : kend);
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const float cl2 = a.scale_log2;
@@ -151,8 +190,9 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
     int i = 0;
     const long rowid = ok ? row_of(g0 + r, i) : 0;
     if (ok) {
-      vis = min(pos0 + gs * i + incl, s1);
+      vis = min(pos0 + gs * i + incl - (WIN ? ws.skip : 0), s1);
       if (DOC) lov = doc_first(a.doc, b, a.T_new, i, pos0 + gs * i);
+      if (WIN) lov = max(pos0 + gs * i + incl - a.window, 0) - ws.skip;
     }
 #pragma unroll
     for (int ks = 0; ks < C::NKS; ++ks)
@@ -176,11 +216,14 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
   // block j of this wave into ring stage st (blocks past the wave's last are copied as
   // zeros, so the count of copies in flight is the same at every wait)
   auto issue = [&](int j, int st) {
-    const uint32_t base =
-        j < nw ? (uint32_t)(s0 + C::BKV * (w + C::NW * j)) * C::ROW_BYTES : kOffOob;
+    const int at = s0 + C::BKV * (w + C::NW * j);
+    const uint32_t base = j < nw ? (uint32_t)at * C::ROW_BYTES : kOffOob;
 #pragma unroll
     for (int n = 0; n < 2 * C::NI; ++n) {
-      const uint32_t o = base + coff[n % C::NI];
+      uint32_t o = base + coff[n % C::NI];
+      if constexpr (WIN)
+        o += at + (64 * (n % C::NI) + lane) / C::CPR >= ws.na ? (uint32_t)ws.skip * C::ROW_BYTES
+                                                              : 0u;
       const uint32_t lds =
           __builtin_amdgcn_readfirstlane(ring_at + st * C::STAGE + 1024 * n);
       if constexpr (ONCE) lds_dma16_stream(lds, o, n < C::NI ? kview : vview);
@@ -188,7 +231,8 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
     }
   };
 
-  const int all_vis = min(pos0 + incl, s1);  // slots below it are visible to every row
+  // slots below it are visible to every row
+  const int all_vis = min(pos0 + incl - (WIN ? ws.skip : 0), s1);
   float m = kNegBig, lsum = 0.f;
   f32x16 o[C::NDT];
 #pragma unroll
@@ -208,14 +252,15 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
 #pragma unroll
     for (int ks = 0; ks < C::NKS; ++ks) sc = mma32(sc, pf_ldk<DH>(ring, lo, kh, ks), qf[ks]);
     const int at = s0 + C::BKV * (w + C::NW * j);  // the block's first slot
-    if (DOC || __builtin_expect(at + C::BKV > all_vis, 0)) {
+    if (DOC || __builtin_expect(at + C::BKV > all_vis ||
+                                (WIN && a.T_new > 1 && at < ws.lo_last), 0)) {
       // some row may not read some of the block's slots
       asm volatile("" : "+v"(vis));  // (keeps the comparisons out of the common path)
       const int base = at + 4 * h;
 #pragma unroll
       for (int q = 0; q < 16; ++q) {
         const int s = base + 8 * (q >> 2) + (q & 3);
-        sc[q] = s >= vis || (DOC && s < lov) ? kNegBig : sc[q];
+        sc[q] = s >= vis || (DOC && s < lov) || (WIN && s < lov && s >= a.sinks) ? kNegBig : sc[q];
       }
     }
     float mx = sc[0];
@@ -314,7 +359,7 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
 }
 
 // ---------------------------------------------- decode on the VALU (fp32, head dim 32)
-template <typename T, int DH, int NG>
+template <typename T, int DH, int NG, bool WIN = false>
 __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
   // A cache slot is read by LPS lanes of 8 elements each.
   constexpr int LPS = DH / 8;
@@ -337,7 +382,10 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
   const int gs = a.gs;
   const int incl = a.mask_paper ? 0 : 1;
   const int kend = min(pos0 + gs * (a.T_new - 1) + incl, a.S_cap);
-  const int s0 = split * a.split_len, s1 = min(s0 + a.split_len, kend);
+  // (WIN: s0, s1 and every slot index below are compact)
+  WindowSpan ws{0, 0, 0, 0};
+  if constexpr (WIN) ws = window_span(pos0 + incl, kend, a.window, a.sinks);
+  const int s0 = split * a.split_len, s1 = min(s0 + a.split_len, WIN ? ws.n : kend);
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int sg = lane / LPS, c8 = lane % LPS;
   const float cl2 = a.scale_log2;
@@ -348,7 +396,8 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
   const __amdgpu_buffer_rsrc_t kview = make_view(a.Kc + cbase, (uint32_t)a.S_cap * DH * sizeof(T));
   const __amdgpu_buffer_rsrc_t vview = make_view(a.Vc + cbase, (uint32_t)a.S_cap * DH * sizeof(T));
   auto slot_off = [&](int s) {
-    return s < s1 ? (uint32_t)(s * DH + 8 * c8) * (uint32_t)sizeof(T) : kOffOob;
+    const int at = WIN && s >= ws.na ? s + ws.skip : s;
+    return s < s1 ? (uint32_t)(at * DH + 8 * c8) * (uint32_t)sizeof(T) : kOffOob;
   };
 
   for (int g0 = 0; g0 < G; g0 += NG) {
@@ -366,8 +415,9 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
         int i = g % a.T_new, gq = (g / a.T_new) % grp, mi = g / (a.T_new * grp);
         int l = a.cg.members[off + mi], hq = kvh * grp + gq;
         long rowid = (((long)l * a.B + b) * a.Hq + hq) * a.T_new + i;
-        vis[gi] = pos0 + gs * i + incl;
-        lov[gi] = doc_first(a.doc, b, a.T_new, i, pos0 + gs * i);
+        vis[gi] = pos0 + gs * i + incl - (WIN ? ws.skip : 0);
+        lov[gi] = WIN ? max(pos0 + gs * i + incl - a.window, 0) - ws.skip
+                      : doc_first(a.doc, b, a.T_new, i, pos0 + gs * i);
         load8(a.Q + rowid * DH + 8 * c8, q[gi]);
       } else {
         vis[gi] = 0;
@@ -400,7 +450,7 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
           for (int i = 0; i < 8; ++i) d += q[gi][i] * to_f32(kr[u][i]);
 #pragma unroll
           for (int x = 1; x < LPS; x <<= 1) d += __shfl_xor(d, x, 64);
-          p[u][gi] = s < s1 && s < vis[gi] && s >= lov[gi] ? d : kNegBig;
+          p[u][gi] = s < s1 && s < vis[gi] && (s >= lov[gi] || (WIN && s < a.sinks)) ? d : kNegBig;
         }
       }
 #pragma unroll
@@ -527,16 +577,22 @@ __global__ __launch_bounds__(256) void attend_combine_kernel(DecodeArgs<T> a) {
     if (active(e)) dst[64 * e + lane] = from_f32<T>(o[e] / Lsum);
 }
 
+template <typename T, int DH, bool WIN>
+static void decode_rows(const DecodeArgs<T>& a, int G, dim3 grid, hipStream_t s) {
+  if (G <= 1)
+    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 1, WIN>), grid, dim3(256), 0, s, a);
+  else if (G <= 2)
+    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 2, WIN>), grid, dim3(256), 0, s, a);
+  else if (G <= 4)
+    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 4, WIN>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 8, WIN>), grid, dim3(256), 0, s, a);
+}
+
 template <typename T, int DH>
 static void decode_dispatch(const DecodeArgs<T>& a, int G, dim3 grid, hipStream_t s) {
-  if (G <= 1)
-    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 1>), grid, dim3(256), 0, s, a);
-  else if (G <= 2)
-    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 2>), grid, dim3(256), 0, s, a);
-  else if (G <= 4)
-    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 4>), grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 8>), grid, dim3(256), 0, s, a);
+  if (a.window > 0) decode_rows<T, DH, true>(a, G, grid, s);
+  else decode_rows<T, DH, false>(a, G, grid, s);
   long rows = (long)a.L * a.B * a.Hq * a.T_new;
   hipLaunchKernelGGL((attend_combine_kernel<T, DH>), dim3((unsigned)((rows + 3) / 4)), dim3(256),
                      0, s, a);
@@ -581,21 +637,24 @@ static void decode_mfma(DecodeArgs<bf16> a, int G, int nlive, const Shape& sh, h
   const long wgs = a.nsplit * slices, per = std::min<long>(kend, len), cus = device_cus();
   const bool four = DH == 96 ? wgs <= cus : wgs <= 2 * cus || (wgs > 5 * cus && per >= 1024);
   const int waves = per <= 128 ? 1 : four ? 4 : 2;
-#define WM_DEC_GO(NW, DOC, ONCE)                                                              \
-  hipLaunchKernelGGL((attend_decode_mfma_kernel<DH, NW, DOC, ONCE>), grid, dim3(64 * (NW)), 0, \
-                     s, a)
-#define WM_DEC_NW(DOC, ONCE)                                                                   \
+#define WM_DEC_GO(NW, DOC, ONCE, WIN)                                                        \
+  hipLaunchKernelGGL((attend_decode_mfma_kernel<DH, NW, DOC, ONCE, WIN>), grid,               \
+                     dim3(64 * (NW)), 0, s, a)
+#define WM_DEC_NW(DOC, ONCE, WIN)                                                              \
   do {                                                                                         \
-    if (waves == 1) WM_DEC_GO(1, DOC, ONCE);                                                   \
-    else if (waves == 2) WM_DEC_GO(2, DOC, ONCE);                                              \
-    else WM_DEC_GO(4, DOC, ONCE);                                                              \
+    if (waves == 1) WM_DEC_GO(1, DOC, ONCE, WIN);                                              \
+    else if (waves == 2) WM_DEC_GO(2, DOC, ONCE, WIN);                                         \
+    else WM_DEC_GO(4, DOC, ONCE, WIN);                                                         \
   } while (0)
   if (a.doc) {
-    if (once) WM_DEC_NW(true, true);
-    else WM_DEC_NW(true, false);
+    if (once) WM_DEC_NW(true, true, false);
+    else WM_DEC_NW(true, false, false);
+  } else if (a.window > 0) {
+    if (once) WM_DEC_NW(false, true, true);
+    else WM_DEC_NW(false, false, true);
   } else {
-    if (once) WM_DEC_NW(false, true);
-    else WM_DEC_NW(false, false);
+    if (once) WM_DEC_NW(false, true, false);
+    else WM_DEC_NW(false, false, false);
   }
 #undef WM_DEC_NW
 #undef WM_DEC_GO
@@ -605,14 +664,17 @@ static void decode_mfma(DecodeArgs<bf16> a, int G, int nlive, const Shape& sh, h
 }
 
 template <typename T>
-void launch_attend_decode(const Shape& sh, const LayerTable& chan_map, const ChannelGroups& cg,
+void launch_attend_decode(const Shape& shape, const LayerTable& chan_map, const ChannelGroups& cg,
                           const T* Q, const T* Kc, const T* Vc, const T* Kd, const T* Vd,
                           const int32_t* ctx_len, const int32_t* doc, float* partials, T* O,
-                          hipStream_t s) {
-  if (sh.N() <= 0) return;
+                          hipStream_t s, const Reach* reach) {
+  if (shape.N() <= 0) return;
+  Shape sh = shape;
+  if (reach) sh.ctx_max = (int)(window_slots(shape, *reach) - shape.span());  // walked slots
   DecodeArgs<T> a{Q, Kc, Vc, Kd, Vd, ctx_len, doc, partials, O, sh.B, sh.T_new, sh.L, sh.Hq, sh.Hkv,
                   sh.S_cap, sh.mask_paper, decode_splits(sh), decode_split_len(sh), sh.gs, sh.gq,
-                  sh.ctx_hi, kLog2e / sqrtf((float)sh.d), chan_map, {}, cg};
+                  sh.ctx_hi, kLog2e / sqrtf((float)sh.d), chan_map, {}, cg,
+                  reach ? reach->window : 0, reach ? reach->sinks : 0};
   int maxmem = 0, nlive = 0;
   for (int c = 0; c < sh.k; ++c) {
     int n = cg.offsets[c + 1] - cg.offsets[c];
@@ -637,7 +699,8 @@ void launch_attend_decode(const Shape& sh, const LayerTable& chan_map, const Cha
 #define WM_INST(T)                                                                              \
   template void launch_attend_decode<T>(const Shape&, const LayerTable&, const ChannelGroups&,  \
                                         const T*, const T*, const T*, const T*, const T*,       \
-                                        const int32_t*, const int32_t*, float*, T*, hipStream_t);
+                                        const int32_t*, const int32_t*, float*, T*, hipStream_t, \
+                                        const Reach*);
 WM_INST(float)
 WM_INST(bf16)
 #undef WM_INST

@@ -130,6 +130,13 @@ template <typename T>
 void launch_group_scatter(const T* Yg, T* Y, int B, int T_len, int g, long row, hipStream_t s);
 
 // -- consumer side (Step 3) ---------------------------------------------------
+// What a row reads besides the dummy: P slots of a prefix common to the batch (Kp, Vp
+// [k][Hkv][P_cap][d]) and, of the cache slots below its limit, the last `window` and the first
+// `sinks`.
+struct Reach {
+  const void *Kp, *Vp;
+  int P, P_cap, window, sinks;
+};
 struct ChannelGroups {       // CSR inverse of the consumer -> channel map
   int offsets[kMaxLayers + 1];
   int members[kMaxLayers];
@@ -270,7 +277,9 @@ template <typename T>
 void launch_attend_decode(const Shape& sh, const LayerTable& chan_map, const ChannelGroups& cg,
                           const T* Q, const T* Kc, const T* Vc, const T* Kd, const T* Vd,
                           const int32_t* ctx_len, const int32_t* doc, float* partials, T* O,
-                          hipStream_t s);
+                          hipStream_t s, const Reach* reach = nullptr);
+long window_slots(const Shape& sh, const Reach& r);
+size_t decode_window_bytes(const Shape& sh);  // the partials with a window (reach)
 
 // The dense soft read: Kl/Vl[l][B][Hkv][S_cap][d] = sum_c w[l][c] Kc/Vc[c], over the slots the
 // call's rows may see, and Kdl/Vdl[l][Hkv][d] from the dummies.
@@ -280,13 +289,6 @@ void launch_soft_read(const Shape& sh, const float* w, const T* Kc, const T* Vc,
                       hipStream_t s);
 
 // -- long contexts (wm_reach.hip, wm_evict.hip) ------------------------------------------
-// What a row reads besides the dummy: P slots of a prefix common to the batch (Kp, Vp
-// [k][Hkv][P_cap][d]) and, of the cache slots below its limit, the last `window` and the first
-// `sinks`.
-struct Reach {
-  const void *Kp, *Vp;
-  int P, P_cap, window, sinks;
-};
 // lse: per row [L][B][Hq][T_new], in log2 units, or null
 template <typename T>
 void launch_reach(const Shape& sh, const Reach& r, const LayerTable& chan, const T* Q, const T* Kc,
