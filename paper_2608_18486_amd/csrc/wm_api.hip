@@ -48,7 +48,7 @@ struct Layout {
   // K/V pre-norm values and gradients, channel gradients, state gradients, logit gradients
   size_t dq = 0, dgp = 0, gkd = 0, x = 0, yq = 0, dyq = 0, dx = 0, hn = 0, u = 0, ydy = 0,
          dyb = 0, du = 0, dhn = 0, dlog = 0, dlogb = 0, split = 0;
-  size_t lse = 0;  // weighed attention: log-sum-exp per row
+  size_t lse = 0, scores = 0;  // weighed attention: per row, and (decode) per row and slot
 };
 
 int group_stride(const wm_dims& d) { return d.groups > 1 ? d.groups : 1; }
@@ -240,10 +240,15 @@ Layout layout(const wm_dims& dd, int op) {
     if (decode_path(d)) Ly.part = take(wm::decode_partials_bytes(dense_shape(make_shape(d))));
   }
   if (layer && decode_path(d)) Ly.part = take(wm::decode_partials_bytes(one_layer(make_shape(d))));
-  if (op == WM_OP_WINDOW_ATTEND && decode_path(d))
-    Ly.part = take(wm::decode_window_bytes(make_shape(d)));
+  if (op == WM_OP_WINDOW_ATTEND || op == WM_OP_WEIGH_ATTEND)
+    Ly.part = take(!decode_path(d) ? wm::kPrefillQueueBytes
+                   : op == WM_OP_WINDOW_ATTEND ? wm::decode_window_bytes(make_shape(d))
+                                               : wm::decode_partials_bytes(make_shape(d)));
   if (op == WM_OP_WINDOW_BACKWARD) Ly.part = take(wm::reach_backward_rows_bytes(make_shape(d)));
-  if (op == WM_OP_WEIGH_ATTEND) Ly.lse = take((size_t)d.L * N * d.Hq * 4);
+  if (op == WM_OP_WEIGH_ATTEND) {
+    Ly.lse = take((size_t)d.L * N * d.Hq * 4);
+    if (decode_path(d)) Ly.scores = take(wm::decode_scores_bytes(make_shape(d)));
+  }
   if (op == WM_OP_CACHE_EVICT) {
     Ly.total = d.B == 0 ? 0 : al256(wm::evict_index_bytes(make_shape(d)));
     return Ly;
@@ -1174,11 +1179,18 @@ wm::Reach window_reach(const wm_dims& d, int32_t window, int32_t sinks) {
   return wm::Reach{nullptr, nullptr, 0, 0, std::min(window, d.S_cap), std::min(sinks, d.S_cap)};
 }
 
+// ctx_len entries past ctx_max act as ctx_max (they size the workspace).
+wm::Shape reach_shape(const wm_dims& d) {
+  wm::Shape sh = make_shape(d);
+  sh.ctx_hi = std::min(sh.ctx_hi, sh.ctx_max);
+  return sh;
+}
+
 template <typename T>
 void run_window(const wm_dims& d, const wm_params& P, const wm::Reach& r, const T* Q,
                 const int32_t* chan_map, const int32_t* ctx_len, const T* Kc, const T* Vc, T* O,
                 void* ws, hipStream_t s) {
-  const wm::Shape sh = make_shape(d);
+  const wm::Shape sh = reach_shape(d);
   const wm::LayerTable mt = map_table(d, chan_map);
   if (decode_path(d))
     wm::launch_attend_decode<T>(sh, mt, groups(d, chan_map), Q, Kc, Vc, (const T*)P.Kd,
@@ -1186,7 +1198,7 @@ void run_window(const wm_dims& d, const wm_params& P, const wm::Reach& r, const 
                                 (float*)at(ws, layout(d, WM_OP_WINDOW_ATTEND).part), O, s, &r);
   else
     wm::launch_reach<T>(sh, r, mt, Q, Kc, Vc, (const T*)P.Kd, (const T*)P.Vd, ctx_len, O, nullptr,
-                        s);
+                        at(ws, layout(d, WM_OP_WINDOW_ATTEND).part), s);
 }
 
 bool overlap(const void* p, size_t n, const void* q, size_t m) {
@@ -1205,22 +1217,43 @@ int check_prefix(const wm_dims& d, int32_t prefix_len, int32_t P_cap) {
 }
 
 size_t shared_ws(const wm_dims& d, int32_t prefix_len) {
-  (void)d;
-  (void)prefix_len;
-  return 0;
+  if ((size_t)d.B * d.T_new == 0) return 0;
+  return al256(decode_path(d) ? wm::decode_shared_bytes(make_shape(d), prefix_len)
+                              : wm::kPrefillQueueBytes);
+}
+
+template <typename T>
+void run_shared(const wm_dims& d, const wm_params& P, const wm::Reach& r, const T* Q,
+                const int32_t* chan_map, const int32_t* ctx_len, const T* Kc, const T* Vc, T* O,
+                void* ws, hipStream_t s) {
+  const wm::Shape sh = reach_shape(d);
+  const wm::LayerTable mt = map_table(d, chan_map);
+  if (decode_path(d))
+    wm::launch_shared_decode<T>(sh, r, mt, groups(d, chan_map), Q, Kc, Vc, (const T*)P.Kd,
+                                (const T*)P.Vd, ctx_len, (float*)ws, O, s);
+  else
+    wm::launch_reach<T>(sh, r, mt, Q, Kc, Vc, (const T*)P.Kd, (const T*)P.Vd, ctx_len, O, nullptr,
+                        ws, s);
 }
 
 template <typename T>
 void run_weigh(const wm_dims& d, const wm_params& P, const T* Q, const int32_t* chan_map,
                       const int32_t* ctx_len, const T* Kc, const T* Vc, T* O, float* weight,
                       void* ws, hipStream_t s) {
-  const wm::Shape sh = make_shape(d);
+  const wm::Shape sh = reach_shape(d);
+  const Layout Ly = layout(d, WM_OP_WEIGH_ATTEND);
+  const wm::LayerTable mt = map_table(d, chan_map);
+  const wm::ChannelGroups cg = groups(d, chan_map);
+  float* lse = (float*)at(ws, Ly.lse);
+  const T *Kd = (const T*)P.Kd, *Vd = (const T*)P.Vd;
+  if (decode_path(d)) {
+    wm::launch_weigh_decode<T>(sh, mt, cg, Q, Kc, Vc, Kd, Vd, ctx_len, (float*)at(ws, Ly.part),
+                               (float*)at(ws, Ly.scores), lse, O, weight, s);
+    return;
+  }
   const wm::Reach r{nullptr, nullptr, 0, 0, d.S_cap, 0};
-  float* lse = (float*)at(ws, layout(d, WM_OP_WEIGH_ATTEND).lse);
-  wm::launch_reach<T>(sh, r, map_table(d, chan_map), Q, Kc, Vc, (const T*)P.Kd, (const T*)P.Vd,
-                      ctx_len, O, lse, s);
-  wm::launch_weigh<T>(sh, map_table(d, chan_map), groups(d, chan_map), Q, Kc, ctx_len, lse,
-                      weight, s);
+  wm::launch_reach<T>(sh, r, mt, Q, Kc, Vc, Kd, Vd, ctx_len, O, lse, at(ws, Ly.part), s);
+  wm::launch_weigh<T>(sh, mt, cg, Q, Kc, ctx_len, lse, weight, s);
 }
 
 }  // namespace
@@ -1825,7 +1858,7 @@ int wm_channel_attend_window_backward(const wm_dims* dims, const wm_params* para
   WM_TRY(need_ptr(dVd, "dVd"));
   WM_TRY(check_ws(d, WM_OP_WINDOW_BACKWARD, ws, ws_bytes));
   (void)hipGetLastError();
-  wm::launch_reach_backward(make_shape(d), window_reach(d, window, sinks), map_table(d, chan_map),
+  wm::launch_reach_backward(reach_shape(d), window_reach(d, window, sinks), map_table(d, chan_map),
                             groups(d, chan_map), (const bf16*)Q, (const bf16*)Kc,
                             (const bf16*)Vc, (const bf16*)params->Kd, (const bf16*)params->Vd,
                             (const bf16*)O, (const bf16*)dO, ctx_len, dQ, dKc, dVc, dKd, dVd,
@@ -1884,13 +1917,11 @@ int wm_channel_attend_shared(const wm_dims* dims, const wm_params* params, const
   const wm::Reach r{Kp, Vp, prefix_len, P_cap, d.S_cap, 0};
   hipStream_t s = (hipStream_t)stream;
   if (d.dtype == WM_BF16)
-    wm::launch_reach<bf16>(make_shape(d), r, map_table(d, chan_map), (const bf16*)Q,
-                           (const bf16*)Kc, (const bf16*)Vc, (const bf16*)params->Kd,
-                           (const bf16*)params->Vd, ctx_len, (bf16*)O, nullptr, s);
+    run_shared<bf16>(d, *params, r, (const bf16*)Q, chan_map, ctx_len, (const bf16*)Kc,
+                     (const bf16*)Vc, (bf16*)O, ws, s);
   else
-    wm::launch_reach<float>(make_shape(d), r, map_table(d, chan_map), (const float*)Q,
-                            (const float*)Kc, (const float*)Vc, (const float*)params->Kd,
-                            (const float*)params->Vd, ctx_len, (float*)O, nullptr, s);
+    run_shared<float>(d, *params, r, (const float*)Q, chan_map, ctx_len, (const float*)Kc,
+                      (const float*)Vc, (float*)O, ws, s);
   return launched();
 }
 

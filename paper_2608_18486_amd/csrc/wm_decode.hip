@@ -70,6 +70,11 @@ template <typename T> struct DecodeArgs {
   LayerTable live;
   ChannelGroups cg;
   int window, sinks;  // WIN kernels: a row reads its last `window` slots and the first `sinks`
+  int split0;         // this kernel's first split among a row's nsplit partial states
+  // weighed attention: raw scores of every row and slot [L][B][Hq][T_new][s_ld] (hidden: -1e30),
+  // and the rows' log-sum-exp in log2 units; else null
+  float *scores, *lse;
+  long s_ld;
 };
 
 // The slots that a sequence's rows read in a window, one after the other: `na` first slots, then
@@ -151,7 +156,7 @@ __device__ __forceinline__ void lds_dma16_stream(uint32_t lds_addr, uint32_t vof
                : "memory", "m0");
 }
 
-template <int DH, int NW, bool DOC, bool ONCE, bool WIN = false>
+template <int DH, int NW, bool DOC, bool ONCE, bool WIN = false, bool SCORES = false>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(3)))
 void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
   using C = DecMfma<DH, NW>;
@@ -185,10 +190,12 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
   };
   int vis = 0, lov = 0;
   bf16x8 qf[C::NKS];
+  float* srow = nullptr;  // SCORES: where this lane's scores go
   {
     const bool ok = g0 + r < G;
     int i = 0;
     const long rowid = ok ? row_of(g0 + r, i) : 0;
+    if (SCORES && ok) srow = a.scores + rowid * a.s_ld + 4 * h;
     if (ok) {
       vis = min(pos0 + gs * i + incl - (WIN ? ws.skip : 0), s1);
       if (DOC) lov = doc_first(a.doc, b, a.T_new, i, pos0 + gs * i);
@@ -263,6 +270,13 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
         sc[q] = s >= vis || (DOC && s < lov) || (WIN && s < lov && s >= a.sinks) ? kNegBig : sc[q];
       }
     }
+    if constexpr (SCORES) {  // rows of s_ld slots, a multiple of 32: no block ends past one
+      if (srow && j < nw) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *(f32x4*)(srow + at + 8 * g) = f32x4{sc[4 * g], sc[4 * g + 1], sc[4 * g + 2], sc[4 * g + 3]};
+      }
+    }
     float mx = sc[0];
 #pragma unroll
     for (int q = 1; q < 16; ++q) mx = fmaxf(mx, sc[q]);
@@ -289,20 +303,8 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
       ps = sum16(p);
     }
     lsum += ps;
-    // a weight's upper 16 bits are its first part; twice more from what is left: 24 bits
     bf16x8 pw[3][2];
-#pragma unroll
-    for (int q = 0; q < 16; q += 2) {
-      uint32_t r0 = __float_as_uint(p[q]), r1 = __float_as_uint(p[q + 1]);
-#pragma unroll
-      for (int u = 0; u < 3; ++u) {
-        const bf16x2 w2 = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(r1, r0, 0x07060302u));
-        pw[u][q >> 3][q & 7] = w2[0];
-        pw[u][q >> 3][(q & 7) + 1] = w2[1];
-        r0 = __float_as_uint(__uint_as_float(r0) - __uint_as_float(r0 & 0xffff0000u));
-        r1 = __float_as_uint(__uint_as_float(r1) - __uint_as_float(r1 & 0xffff0000u));
-      }
-    }
+    cut24(p, pw);
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       bf16x8 vf[C::NDT];
@@ -349,7 +351,7 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
       ow += sw[gi * C::OLD + dd] * al;
     }
     int i;
-    float* dst = a.part + (row_of(g0 + gi, i) * a.nsplit + split) * (DH + 2);
+    float* dst = a.part + (row_of(g0 + gi, i) * a.nsplit + a.split0 + split) * (DH + 2);
     dst[dd] = ow;
     if (dd == 0) {
       dst[DH] = M;
@@ -359,7 +361,7 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
 }
 
 // ---------------------------------------------- decode on the VALU (fp32, head dim 32)
-template <typename T, int DH, int NG, bool WIN = false>
+template <typename T, int DH, int NG, bool WIN = false, bool SCORES = false>
 __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
   // A cache slot is read by LPS lanes of 8 elements each.
   constexpr int LPS = DH / 8;
@@ -403,6 +405,7 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
   for (int g0 = 0; g0 < G; g0 += NG) {
     const int ng = min(NG, G - g0);
     float q[NG][8], m[NG], ls[NG], o[NG][8];
+    float* srow[NG];       // SCORES: where the row's scores go
     int vis[NG], lov[NG];  // the row reads slots lov <= s < vis
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
@@ -418,6 +421,7 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
         vis[gi] = pos0 + gs * i + incl - (WIN ? ws.skip : 0);
         lov[gi] = WIN ? max(pos0 + gs * i + incl - a.window, 0) - ws.skip
                       : doc_first(a.doc, b, a.T_new, i, pos0 + gs * i);
+        if (SCORES) srow[gi] = a.scores + rowid * a.s_ld;
         load8(a.Q + rowid * DH + 8 * c8, q[gi]);
       } else {
         vis[gi] = 0;
@@ -451,6 +455,9 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
 #pragma unroll
           for (int x = 1; x < LPS; x <<= 1) d += __shfl_xor(d, x, 64);
           p[u][gi] = s < s1 && s < vis[gi] && (s >= lov[gi] || (WIN && s < a.sinks)) ? d : kNegBig;
+          if constexpr (SCORES) {
+            if (c8 == 0 && gi < ng && s < s1) srow[gi][s] = p[u][gi];
+          }
         }
       }
 #pragma unroll
@@ -520,7 +527,7 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
       int i = g % a.T_new, gq = (g / a.T_new) % grp, mi = g / (a.T_new * grp);
       int l = a.cg.members[off + mi], hq = kvh * grp + gq;
       long rid = (((long)l * a.B + b) * a.Hq + hq) * a.T_new + i;
-      float* dst = a.part + (rid * a.nsplit + split) * (DH + 2);
+      float* dst = a.part + (rid * a.nsplit + a.split0 + split) * (DH + 2);
       dst[dd] = Osum;
       if (dd == 0) {
         dst[DH] = M;
@@ -575,27 +582,227 @@ __global__ __launch_bounds__(256) void attend_combine_kernel(DecodeArgs<T> a) {
   T* dst = a.O + ((((long)l * a.B + b) * a.T_new + i) * a.Hq + hq) * DH;
   for (int e = 0; e < EPL; ++e)
     if (active(e)) dst[64 * e + lane] = from_f32<T>(o[e] / Lsum);
+  if (a.lse && lane == 0) a.lse[rid] = fmaf(M, cl2, __log2f(Lsum));
 }
 
-template <typename T, int DH, bool WIN>
+// weight[c][b][h][s] += the sum over the rows that read (c, b, h) of 2^(score - lse): a thread takes
+// four slots, the rows' scores as the decode kernel left them.
+template <typename T>
+__global__ __launch_bounds__(256) void decode_weigh_kernel(DecodeArgs<T> a, float* weight) {
+  int y = blockIdx.y;
+  const int kvh = y % a.Hkv;
+  y /= a.Hkv;
+  const int b = y % a.B, ci = y / a.B, c = a.live.v[ci];
+  const int off = a.cg.offsets[ci], nmem = a.cg.offsets[ci + 1] - off, grp = a.Hq / a.Hkv;
+  const int pos0 = ctx_at(a.ctx_len, b, a.ctx_hi) + a.gq;
+  const int kend = min(pos0 + a.gs * (a.T_new - 1) + (a.mask_paper ? 0 : 1), a.S_cap);
+  const int s = 4 * (blockIdx.x * 256 + threadIdx.x);
+  if (s >= kend) return;
+  f32x4 w = {0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < nmem * grp; ++x) {
+    const int l = a.cg.members[off + x / grp], hq = kvh * grp + x % grp;
+    const long row0 = (((long)l * a.B + b) * a.Hq + hq) * a.T_new;
+    for (int i = 0; i < a.T_new; ++i) {
+      const f32x4 sc = *(const f32x4*)(a.scores + (row0 + i) * a.s_ld + s);
+      const float lse = a.lse[row0 + i];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        w[e] += sc[e] > 0.5f * kNegBig ? fast_exp2(fmaf(sc[e], a.scale_log2, -lse)) : 0.f;
+    }
+  }
+  float* dst = weight + (((long)c * a.B + b) * a.Hkv + kvh) * a.S_cap + s;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (s + e < kend) dst[e] += w[e];
+}
+
+// ------------------------------------------------- the shared prefix, few new tokens
+// A prefix slot is read by every sequence, so the rows of one (channel, KV head) are those of the
+// whole batch (consumers x grouped heads x new tokens x sequences), each seeing every slot:
+// products of 32 RT rows per wave against blocks of 32 slots, where a sequence's own cache meets
+// only its own few rows. As in the decode kernel above, a wave walks blocks of its own through a
+// ring of two in LDS; every block it has read serves its RT row tiles, and the row tiles of a
+// split run next to each other on one XCD, whose L2 holds the split's slots for all of them.
+struct PrefixSpan {
+  int P, P_cap, nsplit, split_len, z;  // z: workgroups of 32 RT rows per (slice, split)
+};
+template <int DH, int NW, int RT>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 3 : 2)))
+void attend_prefix_mfma_kernel(DecodeArgs<bf16> a, PrefixSpan px) {
+  using C = DecMfma<DH, NW>;
+  __shared__ __align__(16) char smem[C::NW * C::RING];
+  const int tile = xcd_tile(blockIdx.x, (int)gridDim.x);
+  const int zt = tile % px.z;
+  int y = tile / px.z;
+  const int split = y % px.nsplit;
+  y /= px.nsplit;
+  const int kvh = y % a.Hkv, ci = y / a.Hkv, c = a.live.v[ci];
+  const int off = a.cg.offsets[ci], nmem = a.cg.offsets[ci + 1] - off;
+  const int grp = a.Hq / a.Hkv, per_b = nmem * grp * a.T_new;
+  const int G = per_b * a.B, g0 = 32 * RT * zt;
+  if (g0 >= G) return;
+  const int s0 = split * px.split_len, s1 = min(s0 + px.split_len, px.P);
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const float cl2 = a.scale_log2;
+  auto row_of = [&](int g) {
+    const int b = g / per_b, x = g % per_b, i = x % a.T_new, gq = x / a.T_new % grp;
+    const int l = a.cg.members[off + x / (a.T_new * grp)];
+    return (((long)l * a.B + b) * a.Hq + kvh * grp + gq) * a.T_new + i;
+  };
+  bf16x8 qf[RT][C::NKS];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const bool ok = g0 + 32 * t + r < G;
+    const long rowid = ok ? row_of(g0 + 32 * t + r) : 0;
+#pragma unroll
+    for (int ks = 0; ks < C::NKS; ++ks)
+      qf[t][ks] = ok ? ld_frag<bf16>(a.Q + rowid * DH + 16 * ks + 8 * h) : zero_frag<bf16>();
+  }
+  const int nblk = s1 > s0 ? (s1 - s0 + C::BKV - 1) / C::BKV : 0;
+  const int nw = (nblk - w + C::NW - 1) / C::NW;
+  const long cbase = ((long)c * a.Hkv + kvh) * (long)px.P_cap * DH;
+  const auto kview = make_view(a.Kc + cbase, (uint32_t)px.P * C::ROW_BYTES);
+  const auto vview = make_view(a.Vc + cbase, (uint32_t)px.P * C::ROW_BYTES);
+  uint32_t coff[C::NI];
+#pragma unroll
+  for (int n = 0; n < C::NI; ++n) {
+    const int ch = 64 * n + lane, row = ch / C::CPR;
+    coff[n] = (uint32_t)row * C::ROW_BYTES + 16u * (uint32_t)((ch % C::CPR) ^ pf_swz<DH>(row));
+  }
+  char* ring = smem + w * C::RING;
+  const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
+  auto issue = [&](int j, int st) {
+    const uint32_t base =
+        j < nw ? (uint32_t)(s0 + C::BKV * (w + C::NW * j)) * C::ROW_BYTES : kOffOob;
+#pragma unroll
+    for (int n = 0; n < 2 * C::NI; ++n)
+      lds_dma16(__builtin_amdgcn_readfirstlane(ring_at + st * C::STAGE + 1024 * n),
+                base + coff[n % C::NI], n < C::NI ? kview : vview);
+  };
+  float m[RT], lsum[RT];
+  f32x16 o[RT][C::NDT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    m[t] = kNegBig;
+    lsum[t] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < C::NDT; ++dt) o[t][dt] = zero16();
+  }
+  const PfLane<DH> lo = pf_lane<DH>(lane);
+  issue(0, 0);
+  int j = 0, st = 0;
+  do {
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    issue(j + 1, st ^ 1);
+    wait_copies<2 * C::NI>();
+    const uint32_t kh = st * C::STAGE, vh = kh + C::BLK;
+    const int at = s0 + C::BKV * (w + C::NW * j);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      f32x16 sc = zero16();
+#pragma unroll
+      for (int ks = 0; ks < C::NKS; ++ks) sc = mma32(sc, pf_ldk<DH>(ring, lo, kh, ks), qf[t][ks]);
+      if (__builtin_expect(at + C::BKV > s1, 0)) {
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          sc[q] = at + 4 * h + 8 * (q >> 2) + (q & 3) >= s1 ? kNegBig : sc[q];
+      }
+      float mx = sc[0];
+#pragma unroll
+      for (int q = 1; q < 16; ++q) mx = fmaxf(mx, sc[q]);
+      mx = halves_max(mx);
+      if (__builtin_expect(__any(mx > m[t]), 0)) {
+        const float mn = fmaxf(m[t], mx), al = fast_exp2((m[t] - mn) * cl2);
+        lsum[t] *= al;
+#pragma unroll
+        for (int dt = 0; dt < C::NDT; ++dt) {
+          asm volatile("" : "+v"(o[t][dt]));  // (keeps the products out of the common path)
+          o[t][dt] *= al;
+        }
+        m[t] = mn;
+      }
+      const float mc = m[t] > 0.5f * kNegBig ? m[t] * cl2 : 0.f;
+      f32x16 p;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) p[q] = fast_exp2(fmaf(sc[q], cl2, -mc));
+      lsum[t] += sum16(p);
+      bf16x8 pw[3][2];
+      cut24(p, pw);
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int dt = 0; dt < C::NDT; ++dt) {
+          const bf16x8 vf = pf_ldv<DH>(ring, lo, vh, hf, dt);
+#pragma unroll
+          for (int u = 0; u < 3; ++u) o[t][dt] = mma32(o[t][dt], vf, pw[u][hf]);
+        }
+    }
+    st ^= 1;
+  } while (++j < nw);
+  wait_copies<0>();  // no copy may land in the staging below, or after the block ends
+  // merge the waves' states, a row tile at a time
+  float* so = (float*)ring;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const float lt = halves_sum(lsum[t]);
+#pragma unroll
+    for (int dt = 0; dt < C::NDT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = o[t][dt][4 * g + i];
+        *(f32x4*)(so + r * C::OLD + 32 * dt + 8 * g + 4 * h) = v;
+      }
+    if (h == 0) {
+      so[32 * C::OLD + 2 * r] = m[t];
+      so[32 * C::OLD + 2 * r + 1] = lt;
+    }
+    __syncthreads();
+    const int ng = min(32, G - g0 - 32 * t);
+    for (int e = tid; e < ng * DH; e += C::NT) {
+      const int gi = e / DH, dd = e - gi * DH;
+      float M = kNegBig;
+#pragma unroll
+      for (int ww = 0; ww < C::NW; ++ww)
+        M = fmaxf(M, ((const float*)(smem + ww * C::RING))[32 * C::OLD + 2 * gi]);
+      float lw = 0.f, ow = 0.f;
+#pragma unroll
+      for (int ww = 0; ww < C::NW; ++ww) {
+        const float* sw = (const float*)(smem + ww * C::RING);
+        const float al = fast_exp2((sw[32 * C::OLD + 2 * gi] - M) * cl2);
+        lw += sw[32 * C::OLD + 2 * gi + 1] * al;
+        ow += sw[gi * C::OLD + dd] * al;
+      }
+      float* dst = a.part + (row_of(g0 + 32 * t + gi) * a.nsplit + split) * (DH + 2);
+      dst[dd] = ow;
+      if (dd == 0) {
+        dst[DH] = M;
+        dst[DH + 1] = lw;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T, int DH, bool WIN, bool SCORES>
 static void decode_rows(const DecodeArgs<T>& a, int G, dim3 grid, hipStream_t s) {
   if (G <= 1)
-    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 1, WIN>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 1, WIN, SCORES>), grid, dim3(256), 0, s, a);
   else if (G <= 2)
-    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 2, WIN>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 2, WIN, SCORES>), grid, dim3(256), 0, s, a);
   else if (G <= 4)
-    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 4, WIN>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 4, WIN, SCORES>), grid, dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 8, WIN>), grid, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attend_decode_kernel<T, DH, 8, WIN, SCORES>), grid, dim3(256), 0, s, a);
 }
 
 template <typename T, int DH>
 static void decode_dispatch(const DecodeArgs<T>& a, int G, dim3 grid, hipStream_t s) {
-  if (a.window > 0) decode_rows<T, DH, true>(a, G, grid, s);
-  else decode_rows<T, DH, false>(a, G, grid, s);
-  long rows = (long)a.L * a.B * a.Hq * a.T_new;
-  hipLaunchKernelGGL((attend_combine_kernel<T, DH>), dim3((unsigned)((rows + 3) / 4)), dim3(256),
-                     0, s, a);
+  if (a.scores) decode_rows<T, DH, false, true>(a, G, grid, s);
+  else if (a.window > 0) decode_rows<T, DH, true, false>(a, G, grid, s);
+  else decode_rows<T, DH, false, false>(a, G, grid, s);
 }
 
 // Splits of the matrix-core kernel: slots per workgroup halved (down to decode_split_len,
@@ -614,14 +821,15 @@ constexpr long kDecodeMfmaBlocks = 512;
 constexpr long kDecodeStreamBytes = 128L << 20;
 
 template <int DH>
-static void decode_mfma(DecodeArgs<bf16> a, int G, int nlive, const Shape& sh, hipStream_t s) {
+static void decode_mfma(DecodeArgs<bf16>& a, int G, int nlive, const Shape& sh, hipStream_t s) {
   const int z = std::max(1, (G + 31) / 32);
   const long slices = (long)nlive * sh.B * sh.Hkv * z, kend = (long)sh.ctx_max + sh.span();
   int len = kSplitMax;
   while (len > a.split_len && slices * ((kend + len - 1) / len) < kDecodeMfmaBlocks) len /= 2;
   a.split_len = len;  // at least decode_split_len, so the partials fit their workspace
-  a.nsplit = std::max(1, (int)((kend + len - 1) / len));
-  const dim3 grid(a.nsplit, sh.Hkv * sh.B * nlive, z);
+  const int own = std::max(1, (int)((kend + len - 1) / len));
+  a.nsplit = a.split0 + own;
+  const dim3 grid(own, sh.Hkv * sh.B * nlive, z);
   // a cache read once by one row tile, and larger (all channels: layer by layer, the other
   // layers' calls read theirs in between) than the caches keep from call to call
   const bool once = z == 1 && 4L * sh.k * sh.B * sh.Hkv * kend * DH >= kDecodeStreamBytes;
@@ -634,33 +842,86 @@ static void decode_mfma(DecodeArgs<bf16> a, int G, int nlive, const Shape& sh, h
   // 1000, B 4: 19 / 16.7 / 18.7; ctx 8000, B 1, k = 2: 31 / 26 / 23.6. One layer of 16 heads of
   // 64 with its query, 2 / 4 waves: ctx 700, B 1 19.6 / 19.1; ctx 3000, B 8 38.9 / 33.5; ctx 7948,
   // B 8 62.5 / 57.7; of 12 heads 60.1 / 48.2.
-  const long wgs = a.nsplit * slices, per = std::min<long>(kend, len), cus = device_cus();
+  const long wgs = own * slices, per = std::min<long>(kend, len), cus = device_cus();
   const bool four = DH == 96 ? wgs <= cus : wgs <= 2 * cus || (wgs > 5 * cus && per >= 1024);
   const int waves = per <= 128 ? 1 : four ? 4 : 2;
-#define WM_DEC_GO(NW, DOC, ONCE, WIN)                                                        \
-  hipLaunchKernelGGL((attend_decode_mfma_kernel<DH, NW, DOC, ONCE, WIN>), grid,               \
-                     dim3(64 * (NW)), 0, s, a)
-#define WM_DEC_NW(DOC, ONCE, WIN)                                                              \
+#define WM_DEC_GO(NW, ...)                                                                    \
+  hipLaunchKernelGGL((attend_decode_mfma_kernel<DH, NW, __VA_ARGS__>), grid, dim3(64 * (NW)), \
+                     0, s, a)
+#define WM_DEC_NW(...)                                                                         \
   do {                                                                                         \
-    if (waves == 1) WM_DEC_GO(1, DOC, ONCE, WIN);                                              \
-    else if (waves == 2) WM_DEC_GO(2, DOC, ONCE, WIN);                                         \
-    else WM_DEC_GO(4, DOC, ONCE, WIN);                                                         \
+    if (waves == 1) WM_DEC_GO(1, __VA_ARGS__);                                                 \
+    else if (waves == 2) WM_DEC_GO(2, __VA_ARGS__);                                            \
+    else WM_DEC_GO(4, __VA_ARGS__);                                                            \
   } while (0)
   if (a.doc) {
-    if (once) WM_DEC_NW(true, true, false);
-    else WM_DEC_NW(true, false, false);
+    if (once) WM_DEC_NW(true, true);
+    else WM_DEC_NW(true, false);
+  } else if (a.scores) {
+    if (once) WM_DEC_NW(false, true, false, true);
+    else WM_DEC_NW(false, false, false, true);
   } else if (a.window > 0) {
     if (once) WM_DEC_NW(false, true, true);
     else WM_DEC_NW(false, false, true);
   } else {
-    if (once) WM_DEC_NW(false, true, false);
-    else WM_DEC_NW(false, false, false);
+    if (once) WM_DEC_NW(false, true);
+    else WM_DEC_NW(false, false);
   }
 #undef WM_DEC_NW
 #undef WM_DEC_GO
+}
+
+// Arguments of a call, its channels with a reader in a.live, their number and the most rows of a
+// (channel, sequence, KV head) with them.
+template <typename T>
+static DecodeArgs<T> decode_args(const Shape& sh, const LayerTable& chan_map,
+                                 const ChannelGroups& cg, const T* Q, const T* Kc, const T* Vc,
+                                 const T* Kd, const T* Vd, const int32_t* ctx_len,
+                                 const int32_t* doc, float* partials, T* O, int* nlive, int* G) {
+  DecodeArgs<T> a{Q, Kc, Vc, Kd, Vd, ctx_len, doc, partials, O, sh.B, sh.T_new, sh.L, sh.Hq, sh.Hkv,
+                  sh.S_cap, sh.mask_paper, decode_splits(sh), decode_split_len(sh), sh.gs, sh.gq,
+                  sh.ctx_hi, kLog2e / sqrtf((float)sh.d), chan_map, {}, cg};
+  int maxmem = 0, live = 0;
+  for (int c = 0; c < sh.k; ++c) {
+    int n = cg.offsets[c + 1] - cg.offsets[c];
+    if (n == 0) continue;
+    a.cg.offsets[live] = cg.offsets[c];
+    a.live.v[live++] = c;
+    if (n > maxmem) maxmem = n;
+  }
+  a.cg.offsets[live] = cg.offsets[sh.k];
+  *nlive = live;
+  *G = maxmem * (sh.Hq / sh.Hkv) * sh.T_new;
+  return a;
+}
+
+// The splits' partial states from a.split0 on, and with them the states of a row, a.nsplit.
+template <typename T>
+static void decode_states(DecodeArgs<T>& a, const Shape& sh, int G, int nlive, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {  // fp32 at d = 96 is rejected by validation
+    if (sh.d == 96) return decode_mfma<96>(a, G, nlive, sh, s);
+    if (sh.d == 64) return decode_mfma<64>(a, G, nlive, sh, s);
+  }
+  const dim3 grid(a.nsplit, sh.Hkv * sh.B * nlive);
+  a.nsplit += a.split0;
+  if constexpr (sizeof(T) == 4) {
+    if (sh.d == 64) return decode_dispatch<T, 64>(a, G, grid, s);
+  }
+  decode_dispatch<T, 32>(a, G, grid, s);
+}
+
+template <typename T>
+static void decode_combine(const DecodeArgs<T>& a, int d, hipStream_t s) {
   const long rows = (long)a.L * a.B * a.Hq * a.T_new;
-  hipLaunchKernelGGL((attend_combine_kernel<bf16, DH>), dim3((unsigned)((rows + 3) / 4)),
-                     dim3(256), 0, s, a);
+  const dim3 grid((unsigned)((rows + 3) / 4));
+  if constexpr (sizeof(T) == 2) {
+    if (d == 96) {
+      hipLaunchKernelGGL((attend_combine_kernel<bf16, 96>), grid, dim3(256), 0, s, a);
+      return;
+    }
+  }
+  if (d == 64) hipLaunchKernelGGL((attend_combine_kernel<T, 64>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attend_combine_kernel<T, 32>), grid, dim3(256), 0, s, a);
 }
 
 template <typename T>
@@ -671,36 +932,121 @@ void launch_attend_decode(const Shape& shape, const LayerTable& chan_map, const 
   if (shape.N() <= 0) return;
   Shape sh = shape;
   if (reach) sh.ctx_max = (int)(window_slots(shape, *reach) - shape.span());  // walked slots
-  DecodeArgs<T> a{Q, Kc, Vc, Kd, Vd, ctx_len, doc, partials, O, sh.B, sh.T_new, sh.L, sh.Hq, sh.Hkv,
-                  sh.S_cap, sh.mask_paper, decode_splits(sh), decode_split_len(sh), sh.gs, sh.gq,
-                  sh.ctx_hi, kLog2e / sqrtf((float)sh.d), chan_map, {}, cg,
-                  reach ? reach->window : 0, reach ? reach->sinks : 0};
-  int maxmem = 0, nlive = 0;
-  for (int c = 0; c < sh.k; ++c) {
-    int n = cg.offsets[c + 1] - cg.offsets[c];
-    if (n == 0) continue;
-    a.cg.offsets[nlive] = cg.offsets[c];
-    a.live.v[nlive++] = c;
-    if (n > maxmem) maxmem = n;
+  int nlive, G;
+  DecodeArgs<T> a = decode_args<T>(sh, chan_map, cg, Q, Kc, Vc, Kd, Vd, ctx_len, doc, partials, O,
+                                   &nlive, &G);
+  if (reach) a.window = reach->window, a.sinks = reach->sinks;
+  decode_states<T>(a, sh, G, nlive, s);
+  decode_combine<T>(a, sh.d, s);
+}
+
+// -- weighed
+static long weigh_ld(const Shape& sh) { return ((long)sh.ctx_max + sh.span() + 31) / 32 * 32; }
+size_t decode_scores_bytes(const Shape& sh) {
+  return (size_t)sh.L * sh.N() * sh.Hq * weigh_ld(sh) * sizeof(float);
+}
+
+template <typename T>
+void launch_weigh_decode(const Shape& sh, const LayerTable& chan_map, const ChannelGroups& cg,
+                         const T* Q, const T* Kc, const T* Vc, const T* Kd, const T* Vd,
+                         const int32_t* ctx_len, float* partials, float* scores, float* lse, T* O,
+                         float* weight, hipStream_t s) {
+  if (sh.N() <= 0) return;
+  int nlive, G;
+  DecodeArgs<T> a = decode_args<T>(sh, chan_map, cg, Q, Kc, Vc, Kd, Vd, ctx_len, nullptr, partials,
+                                   O, &nlive, &G);
+  a.scores = scores;
+  a.lse = lse;
+  a.s_ld = weigh_ld(sh);
+  decode_states<T>(a, sh, G, nlive, s);
+  decode_combine<T>(a, sh.d, s);
+  const dim3 grid((unsigned)((a.s_ld / 4 + 255) / 256), (unsigned)(sh.Hkv * sh.B * nlive));
+  hipLaunchKernelGGL(decode_weigh_kernel<T>, grid, dim3(256), 0, s, a, weight);
+}
+
+// -- shared prefix
+// Row tiles of 32 per wave: two where a slice has more than 32 rows (they share every block read).
+static int prefix_tiles(const Shape& sh) {
+  const long rows = (long)sh.L * sh.B * (sh.Hq / sh.Hkv) * sh.T_new / sh.k;
+  return rows > 32 ? 2 : 1;
+}
+// Slots per split of the prefix and its splits, by the dims alone (they size the workspace): as
+// in the decode plan, halved until two workgroups per CU.
+static int prefix_split_len(const Shape& sh, int P) {
+  const long rows = (long)sh.L * sh.B * (sh.Hq / sh.Hkv) * sh.T_new / sh.k;
+  const int per = 32 * prefix_tiles(sh);
+  const long slices = (long)sh.k * sh.Hkv * std::max(1L, (rows + per - 1) / per);
+  int len = kSplitMax;
+  while (len > kSplitMin && slices * ((P + len - 1) / len) < kDecodeMfmaBlocks) len /= 2;
+  return len;
+}
+static int prefix_splits(const Shape& sh, int P) {
+  const int len = prefix_split_len(sh, P);
+  return (P + len - 1) / len;
+}
+size_t decode_shared_bytes(const Shape& sh, int P) {
+  const size_t rows = (size_t)sh.L * sh.B * sh.Hq * sh.T_new;
+  return rows * (decode_splits(sh) + prefix_splits(sh, P)) * (sh.d + 2) * sizeof(float);
+}
+
+template <int DH, int NW, int RT>
+static void prefix_go(const DecodeArgs<bf16>& a, const PrefixSpan& px, int nlive, hipStream_t s) {
+  const dim3 grid((unsigned)(px.z * px.nsplit * a.Hkv * nlive));
+  hipLaunchKernelGGL((attend_prefix_mfma_kernel<DH, NW, RT>), grid, dim3(64 * NW), 0, s, a, px);
+}
+template <int DH>
+static void prefix_states(const DecodeArgs<bf16>& a, PrefixSpan px, int G, int nlive,
+                          const Shape& sh, hipStream_t s) {
+  const int rt = prefix_tiles(sh);
+  px.z = (G * sh.B + 32 * rt - 1) / (32 * rt);
+  // four waves where the workgroups leave CUs to themselves, as in the decode plan
+  const bool four = (long)px.z * px.nsplit * a.Hkv * nlive <= device_cus();
+  if (rt == 2) four ? prefix_go<DH, 4, 2>(a, px, nlive, s) : prefix_go<DH, 2, 2>(a, px, nlive, s);
+  else four ? prefix_go<DH, 4, 1>(a, px, nlive, s) : prefix_go<DH, 2, 1>(a, px, nlive, s);
+}
+
+template <typename T>
+void launch_shared_decode(const Shape& sh, const Reach& r, const LayerTable& chan_map,
+                          const ChannelGroups& cg, const T* Q, const T* Kc, const T* Vc,
+                          const T* Kd, const T* Vd, const int32_t* ctx_len, float* partials, T* O,
+                          hipStream_t s) {
+  if (sh.N() <= 0) return;
+  int nlive, G;
+  DecodeArgs<T> a = decode_args<T>(sh, chan_map, cg, Q, Kc, Vc, Kd, Vd, ctx_len, nullptr, partials,
+                                   O, &nlive, &G);
+  PrefixSpan px{r.P, r.P_cap, prefix_splits(sh, r.P), prefix_split_len(sh, r.P), 1};
+  a.split0 = r.P > 0 ? px.nsplit : 0;
+  decode_states<T>(a, sh, G, nlive, s);
+  if (r.P > 0) {
+    DecodeArgs<T> ap = a;
+    ap.Kc = (const T*)r.Kp;
+    ap.Vc = (const T*)r.Vp;
+    bool done = false;
+    if constexpr (sizeof(T) == 2) {
+      done = sh.d != 32;
+      if (sh.d == 96) prefix_states<96>(ap, px, G, nlive, sh, s);
+      else if (sh.d == 64) prefix_states<64>(ap, px, G, nlive, sh, s);
+    }
+    if (!done)
+      launch_prefix_rows<T>(sh, r, a.live, nlive, a.cg, G * sh.B, Q, partials, a.nsplit, px.nsplit,
+                            px.split_len, s);
   }
-  a.cg.offsets[nlive] = cg.offsets[sh.k];
-  int G = maxmem * (sh.Hq / sh.Hkv) * sh.T_new;
-  dim3 grid(a.nsplit, sh.Hkv * sh.B * nlive);
-  if constexpr (sizeof(T) == 2) {  // fp32 at d = 96 is rejected by validation
-    if (sh.d == 96) decode_mfma<96>(a, G, nlive, sh, s);
-    else if (sh.d == 64) decode_mfma<64>(a, G, nlive, sh, s);
-    else decode_dispatch<T, 32>(a, G, grid, s);
-  } else if (sh.d == 64)
-    decode_dispatch<T, 64>(a, G, grid, s);
-  else
-    decode_dispatch<T, 32>(a, G, grid, s);
+  decode_combine<T>(a, sh.d, s);
 }
 
 #define WM_INST(T)                                                                              \
   template void launch_attend_decode<T>(const Shape&, const LayerTable&, const ChannelGroups&,  \
                                         const T*, const T*, const T*, const T*, const T*,       \
                                         const int32_t*, const int32_t*, float*, T*, hipStream_t, \
-                                        const Reach*);
+                                        const Reach*);                                          \
+  template void launch_weigh_decode<T>(const Shape&, const LayerTable&, const ChannelGroups&,   \
+                                       const T*, const T*, const T*, const T*, const T*,        \
+                                       const int32_t*, float*, float*, float*, T*, float*,      \
+                                       hipStream_t);                                            \
+  template void launch_shared_decode<T>(const Shape&, const Reach&, const LayerTable&,          \
+                                        const ChannelGroups&, const T*, const T*, const T*,     \
+                                        const T*, const T*, const int32_t*, float*, T*,         \
+                                        hipStream_t);
 WM_INST(float)
 WM_INST(bf16)
 #undef WM_INST

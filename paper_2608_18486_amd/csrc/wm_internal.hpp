@@ -281,6 +281,28 @@ void launch_attend_decode(const Shape& sh, const LayerTable& chan_map, const Cha
 long window_slots(const Shape& sh, const Reach& r);
 size_t decode_window_bytes(const Shape& sh);  // the partials with a window (reach)
 
+// The same with the weight every slot receives added to weight [k][B][Hkv][S_cap]; scores:
+// decode_scores_bytes, lse: one float per row.
+size_t decode_scores_bytes(const Shape& sh);
+template <typename T>
+void launch_weigh_decode(const Shape& sh, const LayerTable& chan_map, const ChannelGroups& cg,
+                         const T* Q, const T* Kc, const T* Vc, const T* Kd, const T* Vd,
+                         const int32_t* ctx_len, float* partials, float* scores, float* lse, T* O,
+                         float* weight, hipStream_t s);
+// The same with a prefix of r.P slots common to the batch; partials: decode_shared_bytes.
+size_t decode_shared_bytes(const Shape& sh, int P);
+template <typename T>
+void launch_shared_decode(const Shape& sh, const Reach& r, const LayerTable& chan_map,
+                          const ChannelGroups& cg, const T* Q, const T* Kc, const T* Vc,
+                          const T* Kd, const T* Vd, const int32_t* ctx_len, float* partials, T* O,
+                          hipStream_t s);
+// Partial states of the batch's rows over the prefix (fp32, and bf16 at head dim 32; wm_reach.hip):
+// per live channel at most `rows` rows of a KV head; split i of np into state i of nsplit.
+template <typename T>
+void launch_prefix_rows(const Shape& sh, const Reach& r, const LayerTable& live, int nlive,
+                        const ChannelGroups& cg, int rows, const T* Q, float* part, int nsplit,
+                        int np, int split_len, hipStream_t s);
+
 // The dense soft read: Kl/Vl[l][B][Hkv][S_cap][d] = sum_c w[l][c] Kc/Vc[c], over the slots the
 // call's rows may see, and Kdl/Vdl[l][Hkv][d] from the dummies.
 template <typename T>
@@ -289,11 +311,11 @@ void launch_soft_read(const Shape& sh, const float* w, const T* Kc, const T* Vc,
                       hipStream_t s);
 
 // -- long contexts (wm_reach.hip, wm_evict.hip) ------------------------------------------
-// lse: per row [L][B][Hq][T_new], in log2 units, or null
+// lse: per row [L][B][Hq][T_new], in log2 units, or null; queue: kPrefillQueueBytes
 template <typename T>
 void launch_reach(const Shape& sh, const Reach& r, const LayerTable& chan, const T* Q, const T* Kc,
                   const T* Vc, const T* Kd, const T* Vd, const int32_t* ctx_len, T* O, float* lse,
-                  hipStream_t s);
+                  void* queue, hipStream_t s);
 // weight[k][B][Hkv][S_cap] += the rows' weights on each slot, from their lse
 template <typename T>
 void launch_weigh(const Shape& sh, const LayerTable& chan, const ChannelGroups& cg, const T* Q,

@@ -5,11 +5,25 @@
 //
 // Row (l, b, h, i) sits at position t = ctx_len[b] + gq + gs i; with lim = t (paper mask) or
 // t + 1 (inclusive) it reads every prefix slot, and the cache slots s < lim with s >= lim -
-// window or s < sinks. First form: one wave per row, the head dimension across its lanes.
+// window or s < sinks. A tile of rows walks the slots that any of its rows reads as one compact
+// range x = 0 .. n - 1:
+//   window  its na = min(sinks, lo) first slots, then from its first row's window, lo, on:
+//           slot x < na ? x : x + skip, skip = lo - na. Where skip > 0 every first slot lies
+//           before every row's window, so in compact indexes a row reads x < lim - skip with
+//           x >= lim - window - skip or x < sinks in either case.
+//   prefix  the prefix padded to whole blocks (the pad hidden), then the cache's slots; in the
+//           same terms sinks = P, and lim - window - skip = the padded length for every row.
+// Both are a limit, a lowest slot and a bound of first slots per row (ReachRow).
+//
+// Full-sequence bf16 form at head dims 64 and 96: the pipeline of the prefill attention (128
+// rows per workgroup, K and V blocks of 64 slots through LDS rings of three, S(i + 1) and PV(i -
+// 1) on the matrix cores while the weights of step i are taken). It differs in what it keeps
+// exact: queries enter unscaled, and a weight is exp2(s log2(e) / sqrt(d) - m) from one fma in
+// fp32, where the prefill kernel rounds the scaled queries to bf16 (an error of the weights as
+// large as their own rounding, for one fma per weight less).
 #include <algorithm>
 
-#include "wm_device.hpp"
-#include "wm_internal.hpp"
+#include "wm_prefill.hpp"
 
 namespace wm {
 
@@ -18,53 +32,590 @@ template <typename T> struct ReachArgs {
   const T *Kp, *Vp;  // [k][Hkv][P_cap][d], the shared prefix (P slots)
   const int32_t* ctx_len;
   T* O;
-  float* lse;  // [L][B][Hq][T_new], log2 units, or null
-  int B, T_new, L, Hq, Hkv, S_cap, P, P_cap, window, sinks, mask_paper;
+  float* lse;  // [L][B][Hq][T_new], log2 units (kernels with LSE)
+  int B, T_new, L, Hq, Hkv, S_cap, P, P_cap, window, sinks, mask_paper, n_qtiles;
   int gs, gq, ctx_hi;
   float scale_log2;
-  LayerTable chan;
+  LayerTable chan, lord;  // lord: the consumers in channel order
+  // partial states of the batch's rows over the prefix (FLAT): the channels with a reader and
+  // their consumers, row tiles per slice, states per row, slots per split
+  LayerTable live;
+  ChannelGroups cg;
+  float* part;
+  int z, np, nsplit, split_len;
 };
 
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void reach_rows_kernel(ReachArgs<T> a) {
-  constexpr int E = (DH + 63) / 64;
-  const long rows = (long)a.L * a.B * a.Hq * a.T_new;
-  const long rid = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (rid >= rows) return;
-  const int i = (int)(rid % a.T_new), hq = (int)(rid / a.T_new % a.Hq);
-  const int b = (int)(rid / a.T_new / a.Hq % a.B), l = (int)(rid / a.T_new / a.Hq / a.B);
-  const int c = a.chan.v[l], kvh = hq / (a.Hq / a.Hkv);
-  const int lim = min(ctx_at(a.ctx_len, b, a.ctx_hi) + a.gq + a.gs * i + (a.mask_paper ? 0 : 1),
-                      a.S_cap);
-  const int lo = max(lim - a.window, 0), na = min(a.sinks, lo);
-  float q[E], o[E], m = kNegBig, sum = 0.f;
-  for (int e = 0; e < E; ++e) {
-    q[e] = 64 * e + lane < DH ? to_f32(a.Q[rid * DH + 64 * e + lane]) * a.scale_log2 : 0.f;
-    o[e] = 0.f;
+// The compact range of a tile whose rows' limits run from lim0 to kend (inclusive of both rows).
+struct ReachSpan {
+  int na, skip, n;   // WIN: first slots, slots left out after them, compact slots
+  int low;           // a row reads x >= its limit - low (WIN) or x >= low (prefix)
+  int first;         // ... or x < first
+  int own;           // compact index of cache slot `skip` (prefix: the padded length)
+};
+constexpr int kReachBlk = 64;
+template <typename T, bool PRE>
+__device__ __forceinline__ ReachSpan reach_span(const ReachArgs<T>& a, int lim0, int kend) {
+  ReachSpan r;
+  if constexpr (PRE) {
+    r.own = (a.P + kReachBlk - 1) / kReachBlk * kReachBlk;
+    r.na = r.skip = 0;
+    r.n = r.own + kend;
+    r.low = r.own;
+    r.first = a.P;
+  } else {
+    const int lo = max(lim0 - a.window, 0);
+    r.na = min(a.sinks, lo);
+    r.skip = lo - r.na;
+    r.n = kend - r.skip;
+    r.low = a.window;
+    r.first = a.sinks;
+    r.own = 0;
   }
-  auto slot = [&](const T* kr, const T* vr) {
-    float part = 0.f;
-    for (int e = 0; e < E; ++e)
-      if (64 * e + lane < DH) part += q[e] * to_f32(kr[64 * e + lane]);
-    const float sc = wave_sum(part), mn = fmaxf(m, sc);
-    const float f = fast_exp2(m - mn), p = fast_exp2(sc - mn);
-    sum = sum * f + p;
-    for (int e = 0; e < E; ++e)
-      o[e] = o[e] * f + (64 * e + lane < DH ? p * to_f32(vr[64 * e + lane]) : 0.f);
-    m = mn;
+  return r;
+}
+
+constexpr float kHidden = -__builtin_inff();  // a hidden slot's score: weight 0 at any reference
+
+// Hides the slots of step i (32 from 32 i on) that this lane's row does not read: those at or
+// past lim, and those below lo that are not below first.
+__device__ __forceinline__ void reach_mask(f32x16& v, int i, int lim, int lo, int first, int lane) {
+  const int base = 32 * i + 4 * (lane >> 5);
+  lim -= base, lo -= base, first -= base;
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const int x = 8 * (q >> 2) + (q & 3);
+    v[q] = x >= lim || (x < lo && x >= first) ? kHidden : v[q];
+  }
+}
+
+template <int DH> struct ReachState {  // one wave's running softmax state (2 lanes per row)
+  f32x16 o[DH / 32];  // O^T per 32-column tile of the values
+  bf16x8 pf[2];       // P(i-1)^T fragments
+  float m, lsum;      // reference (log2 units), sum of the weights
+};
+
+// One step of 32 slots: PV(i-1), S(i+1) and the weights of S(i) as independent work of one basic
+// block, in DH / 16 groups whose LDS reads run one group ahead. sc: the raw scores of step i,
+// sn: leaves holding those of step i + 1. LSE: the normaliser adds the weights before their
+// rounding to bf16 (the row statistics are then exact to fp32); else the rounded ones, as the
+// values are weighted.
+template <int DH, bool LSE>
+__device__ __forceinline__ void reach_step(const char* sm, const PfLane<DH>& lo, uint32_t kh_cur,
+                                           uint32_t kh_nxt, uint32_t vh_prv, int i,
+                                           const bf16x8 (&qf)[DH / 16], ReachState<DH>& st,
+                                           f32x16& sc, f32x16& sn, float cl2, int lane, int lim,
+                                           int rlo, int first, bool masked) {
+  if (__builtin_expect(masked, 0)) reach_mask(sc, i, lim, rlo, first, lane);
+  constexpr int NG = DH / 16, NDT = DH / 32;
+  bf16x8 vf[2], kf[2];
+  vf[0] = pf_ldv<DH>(sm, lo, vh_prv, 0, 0);
+  kf[0] = pf_ldk<DH>(sm, lo, kh_nxt, 0);
+  const float mm = -st.m;
+  auto group = [&](auto gc) {
+    constexpr int g = decltype(gc)::value;
+    constexpr int q0 = (16 * g + NG - 1) / NG, q1 = (16 * (g + 1) + NG - 1) / NG;
+    if constexpr (g + 1 < NG) {
+      vf[(g + 1) & 1] = pf_ldv<DH>(sm, lo, vh_prv, (g + 1) / NDT, (g + 1) % NDT);
+      kf[(g + 1) & 1] = pf_ldk<DH>(sm, lo, kh_nxt, g + 1);
+    }
+    st.o[g % NDT] = mma32(st.o[g % NDT], vf[g & 1], st.pf[g / NDT]);
+    sn = mma32(g == 0 ? zero16() : sn, kf[g & 1], qf[g]);
+#pragma unroll
+    for (int q = q0; q < q1; ++q) sc[q] = fast_exp2(fmaf(sc[q], cl2, mm));
+    __builtin_amdgcn_sched_barrier(0);
   };
-  if (a.mask_paper)
-    slot(a.Kd + ((long)c * a.Hkv + kvh) * DH, a.Vd + ((long)c * a.Hkv + kvh) * DH);
-  const long pb = ((long)c * a.Hkv + kvh) * a.P_cap * DH;
-  for (int s = 0; s < a.P; ++s) slot(a.Kp + pb + (long)s * DH, a.Vp + pb + (long)s * DH);
-  const long cb = (((long)c * a.B + b) * a.Hkv + kvh) * a.S_cap * DH;
-  for (int s = 0; s < na; ++s) slot(a.Kc + cb + (long)s * DH, a.Vc + cb + (long)s * DH);
-  for (int s = lo; s < lim; ++s) slot(a.Kc + cb + (long)s * DH, a.Vc + cb + (long)s * DH);
-  T* dst = a.O + ((((long)l * a.B + b) * a.T_new + i) * a.Hq + hq) * DH;
-  for (int e = 0; e < E; ++e)
-    if (64 * e + lane < DH) dst[64 * e + lane] = from_f32<T>(o[e] / sum);
-  if (a.lse && lane == 0) a.lse[rid] = m + __log2f(sum);
+  static_for<0, NG>(group);
+#pragma unroll
+  for (int q = 0; q < 16; ++q) st.pf[q >> 3][q & 7] = (bf16)sc[q];
+  float ps = LSE ? tree_sum<0, 16>(sc) : pf_wsum(st.pf[0], st.pf[1]);
+  if (__builtin_expect(__any(!(ps <= kGrowSum) || st.m == kNoRef), 0)) {
+    // rare: the reference moves to the exact row maximum (never down, but from kNoRef to it)
+    f32x16 sr = pf_scores<DH>(sm, lo, kh_cur, qf, zero16());
+    if (masked) reach_mask(sr, i, lim, rlo, first, lane);
+    float mx = sr[0];
+#pragma unroll
+    for (int q = 1; q < 16; ++q) mx = fmaxf(mx, sr[q]);
+    const float grow = ref_growth(fmaf(halves_max(mx), cl2, -st.m), st.m);
+    const float alpha = ref_rescale(grow, st.m);
+    st.m += grow;
+    st.lsum *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) st.o[dt] *= alpha;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      sr[q] = fast_exp2(fmaf(sr[q], cl2, -st.m));
+      st.pf[q >> 3][q & 7] = (bf16)sr[q];
+    }
+    ps = LSE ? tree_sum<0, 16>(sr) : pf_wsum(st.pf[0], st.pf[1]);
+  }
+  st.lsum += ps;
+}
+
+// One tile: 32 rows per wave of one (consumer, sequence, query head). On entry every wave is past
+// the previous tile.
+template <int DH, bool PRE, bool LSE>
+__device__ __forceinline__ void reach_tile(const ReachArgs<bf16>& a, const int tile, char* smem) {
+  using P = PfDma<1, DH>;
+  constexpr int NKS = P::NKS, NDT = P::NDT;
+  // tile order: sequence, KV head, consumer (in channel order), grouped head, query tile (last
+  // first): consecutive tiles read neighbouring slots of one K/V slice
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.Hq / a.Hkv;
+  const int qtile = a.n_qtiles - 1 - tile % a.n_qtiles;
+  int y = tile / a.n_qtiles;
+  const int hg = y % G;
+  y /= G;
+  const int li = y % a.L;
+  y /= a.L;
+  const int kvh = y % a.Hkv, b = y / a.Hkv;
+  const int hq = kvh * G + hg, l = a.lord.v[li], c = a.chan.v[l];
+  const int pos0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq;
+  const int incl = a.mask_paper ? 0 : 1, gs = a.gs;
+  const int q0 = qtile * P::BQ, qw0 = q0 + 32 * w, qi = qw0 + r;
+  const float cl2 = a.scale_log2;
+
+  bf16x8 qf[NKS];
+  {
+    const auto qview = make_view(a.Q + (((long)l * a.B + b) * a.Hq + hq) * (long)a.T_new * DH,
+                                 (uint32_t)a.T_new * DH * 2u);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+      qf[ks] = buf_frag<bf16>(qview, qi < a.T_new ? (uint32_t)(qi * DH + 16 * ks + 8 * h) * 2u
+                                                  : kOffOob);
+  }
+  bf16x8 kdv[NKS];
+  bf16x4 vdv[NDT][4];
+  {
+    const long dof = ((long)c * a.Hkv + kvh) * DH;
+    const uint32_t dbytes = a.mask_paper ? DH * 2u : 0u;
+    const auto kdview = make_view(a.mask_paper ? a.Kd + dof : nullptr, dbytes);
+    const auto vdview = make_view(a.mask_paper ? a.Vd + dof : nullptr, dbytes);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) kdv[ks] = buf_frag<bf16>(kdview, (16 * ks + 8 * h) * 2u);
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4)
+        vdv[dt][g4] = buf_ld8(vdview, (32 * dt + 8 * g4 + 4 * h) * 2u);
+  }
+
+  const int qlast = min(q0 + P::BQ, a.T_new) - 1;
+  const int kend = min(pos0 + gs * qlast + incl, a.S_cap);  // cache slots the tile may see
+  const ReachSpan sp = reach_span<bf16, PRE>(a, pos0 + gs * q0 + incl, kend);
+  const int nblk = (sp.n + P::BKV - 1) / P::BKV;
+  // compact limits: this lane's row, the wave's first and last row
+  const int off = pos0 + incl + sp.own - sp.skip;
+  const int lim = off + gs * qi, wlim0 = off + gs * qw0;
+  const int wlast = min(qw0 + 31, a.T_new - 1), wlim1 = off + gs * wlast;
+  const int rlo = PRE ? sp.low : lim - sp.low;
+  const int wlo0 = PRE ? sp.low : wlim0 - sp.low, wlo1 = PRE ? sp.low : wlim1 - sp.low;
+  // a step is unmasked where every row of the wave reads all of it
+  auto masked = [&](int i) {
+    return 32 * i + 32 > wlim0 || (32 * i < wlo1 && 32 * i + 32 > sp.first);
+  };
+  const int ilast = wlast >= qw0 ? (wlim1 + 31) / 32 - 1 : -2;  // the wave's last step
+  // Steps that no row of the wave reads, between the first slots and its lowest window, are
+  // skipped: it runs steps 0 .. a2 (the last one only to add the PV of the step before) and
+  // starts again at step r0, with the scores of r0 taken anew.
+  const int a2 = sp.first > 0 ? 2 * ((min(sp.first, sp.n) + 63) / 64) : 0;
+  int r0 = PRE ? 0 : max(wlo0, 0) / 64 * 2;
+  if (r0 <= a2 && a2 > 0) r0 = 0;
+  const bool gap = r0 > 0;
+
+  const long cbase = (((long)c * a.B + b) * a.Hkv + kvh) * (long)a.S_cap * DH;
+  const auto kview = make_view(a.Kc + cbase, (uint32_t)max(kend, 0) * P::ROW_BYTES);
+  const auto vview = make_view(a.Vc + cbase, (uint32_t)max(kend, 0) * P::ROW_BYTES);
+  const long pbase = PRE ? ((long)c * a.Hkv + kvh) * (long)a.P_cap * DH : 0;
+  const uint32_t pbytes = PRE ? (uint32_t)a.P * P::ROW_BYTES : 0u;
+  const auto kpview = make_view(PRE ? a.Kp + pbase : nullptr, pbytes);
+  const auto vpview = make_view(PRE ? a.Vp + pbase : nullptr, pbytes);
+  const int pblk = sp.own / P::BKV;
+  uint32_t coff[P::NI];  // byte offset of the lane's chunk within block 0
+  int crow0[P::NI];
+#pragma unroll
+  for (int n = 0; n < P::NI; ++n) {
+    const int ch = 64 * n + lane, crow = P::RPW * w + ch / P::CPR;
+    crow0[n] = crow;
+    coff[n] = (uint32_t)crow * P::ROW_BYTES + 16u * (uint32_t)((ch % P::CPR) ^ pf_swz<DH>(crow));
+  }
+  const uint32_t smem_base = (uint32_t)(uintptr_t)smem;
+  // blocks past the range are copied as zeros, so that every wave issues the same sequence (K0
+  // K1 V0 | K2 V1 | K3 V2 | ...) and one vmcnt fits every block
+  auto issue = [&](int blk, bool v) {
+    const bool pre = PRE && blk < pblk;
+#pragma unroll
+    for (int n = 0; n < P::NI; ++n) {
+      uint32_t o = coff[n] + (uint32_t)(pre || !PRE ? blk : blk - pblk) * P::BLK_BYTES;
+      if constexpr (!PRE)
+        o += blk * P::BKV + crow0[n] >= sp.na ? (uint32_t)sp.skip * P::ROW_BYTES : 0u;
+      const uint32_t lds = __builtin_amdgcn_readfirstlane(
+          smem_base + (v ? P::V_BASE : 0) + (blk % P::NS) * P::BLK_BYTES +
+          P::RPW * w * P::ROW_BYTES + 1024 * n);
+      if constexpr (PRE) lds_dma16(lds, o, pre ? (v ? vpview : kpview) : (v ? vview : kview));
+      else lds_dma16(lds, o, v ? vview : kview);
+    }
+  };
+  static_assert(P::NS == 3, "the counts of copies in flight below");
+  // the first step's PV has no block before it: its (weightless) values are zeros, not what an
+  // earlier tile of another sequence left there
+  for (int x = 16 * tid; x < 32 * P::ROW_BYTES; x += 16 * P::NT)
+    *(i32x4*)(smem + pf_vh<DH>(2, 1) + x) = i32x4{0, 0, 0, 0};
+  issue(0, false);
+  issue(1, false);
+  issue(0, true);
+
+  ReachState<DH> st;
+  f32x16 sa, sb;  // scores of even and odd steps
+  st.pf[0] = st.pf[1] = zero_frag<bf16>();
+  if (a.mask_paper) {
+    float part = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part += (float)qf[ks][i] * (float)kdv[ks][i];
+    st.m = halves_sum(part) * cl2;
+    st.lsum = h == 0 ? 1.f : 0.f;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) st.o[dt][q] = (float)vdv[dt][q >> 2][q & 3];
+  } else {
+    st.m = kNoRef;
+    st.lsum = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) st.o[dt] = zero16();
+  }
+  sa = sb = zero16();
+  wait_vmcnt<P::NI * 2>();
+  __syncthreads();
+  PfLane<DH> lo = pf_lane<DH>(lane);
+  auto runs = [&](int i) { return i <= ilast + 1 && (!gap || i < a2 + (a2 > 0) || i >= r0); };
+  auto block = [&](const int j, auto uc) {
+    constexpr int u = decltype(uc)::value;
+    // keep the lane offsets as they are (not one precomputed address per use)
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+v"(lo.k[ks]));
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) asm volatile("" : "+v"(lo.v[dt][0]), "+v"(lo.v[dt][1]));
+    // every wave is past block j-1: the stages of K(j-1) and V(j-2) are free
+    __syncthreads();
+    issue(j + P::NS - 1, false);
+    issue(j + P::NS - 2, true);
+    const int i = 2 * j;
+    if ((j == 0 || (gap && i == r0)) && i <= ilast)
+      sa = pf_scores<DH>(smem, lo, pf_kh<DH>(u, 0), qf, zero16());
+    // steps up to ilast + 1: the last one only adds PV(ilast)
+    if (runs(i))
+      reach_step<DH, LSE>(smem, lo, pf_kh<DH>(u, 0), pf_kh<DH>(u, 1),
+                          pf_vh<DH>((u + P::NS - 1) % P::NS, 1), i, qf, st, sa, sb, cl2, lane, lim,
+                          rlo, sp.first, masked(i));
+    wait_vmcnt<2 * P::NI>();  // K(j+1) and V(j) have landed
+    __syncthreads();
+    if (runs(i + 1))
+      reach_step<DH, LSE>(smem, lo, pf_kh<DH>(u, 1), pf_kh<DH>((u + 1) % P::NS, 0), pf_vh<DH>(u, 0),
+                          i + 1, qf, st, sb, sa, cl2, lane, lim, rlo, sp.first, masked(i + 1));
+  };
+  for (int j = 0; j < nblk; j += P::NS) {
+    block(j, std::integral_constant<int, 0>());
+    if (j + 1 < nblk) block(j + 1, std::integral_constant<int, 1>());
+    if (j + 2 < nblk) block(j + 2, std::integral_constant<int, 2>());
+  }
+  if (ilast + 1 == 2 * nblk && runs(2 * nblk)) {
+    const int u = nblk % P::NS;
+    reach_step<DH, LSE>(smem, lo, pf_kh<DH>(u, 0), pf_kh<DH>(u, 1),
+                        pf_vh<DH>((u + P::NS - 1) % P::NS, 1), 2 * nblk, qf, st, sa, sb, cl2, lane,
+                        lim, rlo, sp.first, true);
+  }
+  wait_vmcnt<0>();  // no copy may land after the workgroup ends
+
+  const float lt = halves_sum(st.lsum);
+  if (qi < a.T_new) {
+    const float inv = 1.0f / lt;
+    bf16* dst = a.O + ((((long)l * a.B + b) * a.T_new + qi) * a.Hq + hq) * DH;
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = st.o[dt][4 * g + i] * inv;
+        store4(dst + 32 * dt + 8 * g + 4 * h, v);
+      }
+    if (LSE && h == 0)
+      a.lse[(((long)l * a.B + b) * a.Hq + hq) * a.T_new + qi] = st.m + __log2f(lt);
+  }
+}
+
+// Grid and work queue as the prefill kernel's (attend_prefill_dma_kernel): one workgroup per tile
+// where the CUs hold them all at once, else as many as they hold, each XCD's taking tiles of its
+// contiguous share from a counter (queue, reset on the stream before).
+template <int DH, bool PRE, bool LSE>
+__global__ __launch_bounds__(64 * kPfWaves) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 3 : 2)))
+void reach_dma_kernel(ReachArgs<bf16> a, uint32_t* queue) {
+  using P = PfDma<1, DH>;
+  __shared__ __align__(16) char smem[P::SMEM_BYTES];
+  __shared__ int s_tile;
+  const int tid = threadIdx.x;
+  const int total = a.n_qtiles * a.Hq * a.B * a.L;
+  if (!queue) {
+    reach_tile<DH, PRE, LSE>(a, xcd_tile(blockIdx.x, total), smem);
+    return;
+  }
+  const int nq = min((int)gridDim.x, kNumXcd), x = blockIdx.x % nq;
+  const int per = total / nq, rem = total % nq;
+  const int first = x * per + min(x, rem), count = per + (x < rem ? 1 : 0);
+  uint32_t* ctr = queue + kQueueStride * x;
+  if (tid == 0) s_tile = (int)atomicAdd(ctr, 1u);
+  __syncthreads();
+  int t = __builtin_amdgcn_readfirstlane(s_tile);
+  while (t < count) {
+    reach_tile<DH, PRE, LSE>(a, first + t, smem);
+    if (tid == 0) s_tile = (int)atomicAdd(ctr, 1u);
+    __syncthreads();
+    t = __builtin_amdgcn_readfirstlane(s_tile);
+  }
+}
+
+__global__ void reach_queue_kernel(uint32_t* queue) { queue[threadIdx.x] = 0u; }
+
+// ------------------------------------------- fp32, and bf16 at head dim 32
+// The same tiles without the pipeline: 256 rows per workgroup (8 waves of 32), K and V blocks of
+// 64 slots double-buffered in LDS through registers, V transposed for fp32 (whose matrix
+// instructions have no transposing read). fp32 products run on the fp32 matrix cores, an eighth of
+// the bf16 rate, which bounds this form. FLAT: the rows are the batch's rows of one (channel, KV
+// head) side by side, the slots a split of the prefix, the result a partial state per row.
+template <typename T, int DH, bool PRE, bool LSE, bool FLAT = false>
+__global__ __launch_bounds__(64 * kPrefillWaves) void reach_prefill_kernel(ReachArgs<T> a) {
+  using C = PrefillCfg<T, DH>;
+  static_assert(C::QT == 1, "one tile of 32 rows per wave");
+  __shared__ __align__(16) T Ks[2][C::BKV * C::LDK];
+  __shared__ __align__(16) T Vt[2][C::VS];
+  const int tile = xcd_tile(blockIdx.x, (int)gridDim.x);
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, h = lane >> 5, r = lane & 31;
+  const float cl2 = a.scale_log2;
+  int l = 0, b = 0, hq = 0, kvh, c, q0, kend = 0, split = 0, rows = a.T_new;
+  int off = 0, lim, wlim0, wlim1, rlo, wlo0, wlo1;
+  ReachSpan sp{};
+  long qrow = 0;  // this lane's row of Q
+  if constexpr (FLAT) {
+    int y = tile / a.z;
+    q0 = tile % a.z * C::BQ;
+    split = y % a.np;
+    y /= a.np;
+    kvh = y % a.Hkv;
+    const int ci = y / a.Hkv, grp = a.Hq / a.Hkv;
+    c = a.live.v[ci];
+    const int per_b = (a.cg.offsets[ci + 1] - a.cg.offsets[ci]) * grp * a.T_new;
+    rows = per_b * a.B;
+    if (q0 >= rows) return;
+    const int g = min(q0 + 32 * w + r, rows - 1), x = g % per_b, gl = x / a.T_new;
+    const int ml = a.cg.members[a.cg.offsets[ci] + gl / grp];
+    qrow = (((long)ml * a.B + g / per_b) * a.Hq + kvh * grp + gl % grp) * a.T_new + x % a.T_new;
+    sp.own = (a.P + kReachBlk - 1) / kReachBlk * kReachBlk;  // every slot walked is the prefix's
+    sp.n = lim = wlim0 = wlim1 = min((split + 1) * a.split_len, a.P);
+    rlo = wlo0 = wlo1 = 0;
+  } else {
+    const int qtile = a.n_qtiles - 1 - tile % a.n_qtiles;
+    int y = tile / a.n_qtiles;
+    hq = y % a.Hq;
+    y /= a.Hq;
+    b = y % a.B, l = y / a.B;
+    c = a.chan.v[l], kvh = hq / (a.Hq / a.Hkv);
+    q0 = qtile * C::BQ;
+    qrow = (((long)l * a.B + b) * a.Hq + hq) * a.T_new + min(q0 + 32 * w + r, a.T_new - 1);
+    const int pos0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq;
+    const int incl = a.mask_paper ? 0 : 1, gs = a.gs;
+    const int qlast = min(q0 + C::BQ, a.T_new) - 1;
+    kend = min(pos0 + gs * qlast + incl, a.S_cap);
+    sp = reach_span<T, PRE>(a, pos0 + gs * q0 + incl, kend);
+    off = pos0 + incl + sp.own - sp.skip;
+    const int wl = q0 + 32 * w;
+    lim = off + gs * (wl + r), wlim0 = off + gs * wl;
+    wlim1 = off + gs * min(wl + 31, a.T_new - 1);
+    rlo = PRE ? sp.low : lim - sp.low;
+    wlo0 = PRE ? sp.low : wlim0 - sp.low, wlo1 = PRE ? sp.low : wlim1 - sp.low;
+  }
+  const int qw0 = q0 + 32 * w, qi = qw0 + r;
+  const int j0 = FLAT ? split * a.split_len / C::BKV : 0, nblk = (sp.n + C::BKV - 1) / C::BKV;
+  const bool live = qw0 < rows;
+
+  frag_t<T> qf[C::NKS];
+#pragma unroll
+  for (int ks = 0; ks < C::NKS; ++ks)
+    qf[ks] = qi < rows ? ld_frag<T>(a.Q + qrow * DH + 16 * ks + 8 * h) : zero_frag<T>();
+  float m = kNoRef, lsum = 0.f;
+  f32x16 o[C::NDT];
+#pragma unroll
+  for (int dt = 0; dt < C::NDT; ++dt) o[dt] = zero16();
+  if (!FLAT && a.mask_paper) {
+    const T* kd = a.Kd + ((long)c * a.Hkv + kvh) * DH;
+    const T* vd = a.Vd + ((long)c * a.Hkv + kvh) * DH;
+    float part = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < C::NKS; ++ks)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part += to_f32(qf[ks][i]) * to_f32(kd[16 * ks + 8 * h + i]);
+    m = halves_sum(part) * cl2;
+    lsum = h == 0 ? 1.f : 0.f;
+#pragma unroll
+    for (int dt = 0; dt < C::NDT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) o[dt][q] = to_f32(vd[32 * dt + 8 * (q >> 2) + 4 * h + (q & 3)]);
+  }
+
+  const long cbase = (((long)c * a.B + b) * a.Hkv + kvh) * (long)a.S_cap * DH;
+  const auto kview = make_view(FLAT ? nullptr : a.Kc + cbase,
+                               FLAT ? 0u : (uint32_t)a.S_cap * DH * sizeof(T));
+  const auto vview = make_view(FLAT ? nullptr : a.Vc + cbase,
+                               FLAT ? 0u : (uint32_t)a.S_cap * DH * sizeof(T));
+  const long pbase = PRE ? ((long)c * a.Hkv + kvh) * (long)a.P_cap * DH : 0;
+  const uint32_t pbytes = PRE ? (uint32_t)a.P * DH * sizeof(T) : 0u;
+  const auto kpview = make_view(PRE ? a.Kp + pbase : nullptr, pbytes);
+  const auto vpview = make_view(PRE ? a.Vp + pbase : nullptr, pbytes);
+  frag_t<T> kreg[C::KFR], vreg[C::VPT][C::VTR ? 1 : 2];
+  // compact slot x of a block that lies in the prefix (pre) or in the cache
+  auto slot_off = [&](int x, int col, bool pre) {
+    const int s = PRE ? (pre ? x : x - sp.own) : x < sp.na ? x : x + sp.skip;
+    const bool ok = PRE && pre ? s < a.P : s < kend;
+    return ok ? (uint32_t)(s * DH + col) * (uint32_t)sizeof(T) : kOffOob;
+  };
+  auto fetch = [&](int k0) {
+    const bool pre = PRE && k0 < sp.own;
+    const auto kv = PRE && pre ? kpview : kview, vv = PRE && pre ? vpview : vview;
+#pragma unroll
+    for (int i = 0; i < C::KFR; ++i) {
+      const int f = tid + C::NT * i, key = f / (DH / 8), dc = (f % (DH / 8)) * 8;
+      kreg[i] = buf_frag<T>(kv, f < C::KIT ? slot_off(k0 + key, dc, pre) : kOffOob);
+    }
+#pragma unroll
+    for (int i = 0; i < C::VPT; ++i) {
+      const int it = tid + C::NT * i;
+      const bool ok = it < C::VIT;
+      if constexpr (C::VTR) {
+        const int key = it / (DH / 8), dc = (it % (DH / 8)) * 8;
+        vreg[i][0] = buf_frag<T>(vv, ok ? slot_off(k0 + key, dc, pre) : kOffOob);
+      } else {
+        const int kp = it % (C::BKV / 2), dg = it / (C::BKV / 2), x = k0 + 2 * kp;
+        vreg[i][0] = buf_frag<T>(vv, ok ? slot_off(x, 8 * dg, pre) : kOffOob);
+        vreg[i][1] = buf_frag<T>(vv, ok ? slot_off(x + 1, 8 * dg, pre) : kOffOob);
+      }
+    }
+  };
+  auto stage = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < C::KFR; ++i) {
+      const int f = tid + C::NT * i, key = f / (DH / 8), dc = (f % (DH / 8)) * 8;
+      if (f < C::KIT) st_frag<T>(&Ks[buf][key * C::LDK + dc], kreg[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < C::VPT; ++i) {
+      const int it = tid + C::NT * i;
+      if (it < C::VIT) {
+        if constexpr (C::VTR) {
+          const int key = it / (DH / 8), dc = (it % (DH / 8)) * 8;
+          st_frag<T>(&Vt[buf][key * C::LDV + dc], vreg[i][0]);
+        } else {
+          const int kp = it % (C::BKV / 2), dg = it / (C::BKV / 2);
+          st_pair_t(&Vt[buf][(8 * dg) * C::LDV + 2 * kp], C::LDV, vreg[i][0], vreg[i][1]);
+        }
+      }
+    }
+  };
+  // half a block (32 slots from x0 on) against the wave's rows
+  auto half = [&](int x0, int kt, const T* ks_, const T* vt_) {
+    f32x16 sc = zero16();
+#pragma unroll
+    for (int ks = 0; ks < C::NKS; ++ks)
+      sc = mma32(sc, ld_frag<T>(ks_ + (32 * kt + r) * C::LDK + 16 * ks + 8 * h), qf[ks]);
+    if (x0 + 32 > wlim0 || (x0 < wlo1 && x0 + 32 > sp.first))
+      reach_mask(sc, x0 / 32, lim, rlo, sp.first, lane);
+    f32x16 pv;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) pv[q] = fast_exp2(fmaf(sc[q], cl2, -m));
+    float ps = tree_sum<0, 16>(pv);
+    if (__any(!(ps <= kGrowSum) || m == kNoRef)) {  // rare, as in the pipelined form
+      float mx = sc[0];
+#pragma unroll
+      for (int q = 1; q < 16; ++q) mx = fmaxf(mx, sc[q]);
+      const float grow = ref_growth(fmaf(halves_max(mx), cl2, -m), m);
+      const float alpha = ref_rescale(grow, m);
+      m += grow;
+      lsum *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < C::NDT; ++dt) o[dt] *= alpha;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) pv[q] = fast_exp2(fmaf(sc[q], cl2, -m));
+      ps = tree_sum<0, 16>(pv);
+    }
+    lsum += ps;
+    // bf16: the few tokens of FLAT calls keep the weights' 24 bits, as their other slots do
+    constexpr int NP = FLAT && sizeof(T) == 2 ? 3 : 1;
+    frag_t<T> pf[NP][2];
+    if constexpr (NP == 3) {
+      cut24(pv, pf);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) pf[0][q >> 3][q & 7] = from_f32<T>(pv[q]);
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int kc = 32 * kt + 16 * hf + 4 * h;
+#pragma unroll
+      for (int dt = 0; dt < C::NDT; ++dt) {
+        frag_t<T> vf;
+        if constexpr (C::VTR) {
+          vf = ld_vt_tr(vt_, C::LDV, 32 * kt + 16 * hf, dt, 32 * h + r);
+        } else {
+          const T* vrow = vt_ + (32 * dt + r) * C::LDV;
+          vf = ld_frag_4_4<T>(vrow + kc, vrow + kc + 8);
+        }
+#pragma unroll
+        for (int u = 0; u < NP; ++u) o[dt] = mma32(o[dt], vf, pf[u][hf]);
+      }
+    }
+  };
+  fetch(j0 * C::BKV);
+  stage(j0 & 1);
+  __syncthreads();
+  for (int j = j0; j < nblk; ++j) {
+    const int k0 = j * C::BKV, buf = j & 1;
+    fetch(k0 + C::BKV);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      const int x0 = k0 + 32 * kt;
+      // wave-uniform: some row may read some of the 32 slots
+      if (live && x0 < wlim1 && (x0 + 32 > wlo0 || x0 < sp.first)) half(x0, kt, Ks[buf], Vt[buf]);
+    }
+    stage(buf ^ 1);
+    __syncthreads();
+  }
+  const float lt = halves_sum(lsum);
+  if (qi >= rows) return;
+  if constexpr (FLAT) {  // the decode kernels' partial state: o unnormalised, m in score units, l
+    float* dst = a.part + (qrow * a.nsplit + split) * (DH + 2);
+#pragma unroll
+    for (int dt = 0; dt < C::NDT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) dst[32 * dt + 8 * (q >> 2) + 4 * h + (q & 3)] = o[dt][q];
+    if (h == 0) {
+      dst[DH] = m / cl2;
+      dst[DH + 1] = lt;
+    }
+    return;
+  }
+  const float inv = 1.0f / lt;
+  T* dst = a.O + ((((long)l * a.B + b) * a.T_new + qi) * a.Hq + hq) * DH;
+#pragma unroll
+  for (int dt = 0; dt < C::NDT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = o[dt][4 * g + i] * inv;
+      store4(dst + 32 * dt + 8 * g + 4 * h, v);
+    }
+  if (LSE && h == 0) a.lse[(((long)l * a.B + b) * a.Hq + hq) * a.T_new + qi] = m + __log2f(lt);
 }
 
 // weight[c][b][kvh][s] += sum of exp2(score - lse) over the rows that read the slot: a wave per
@@ -96,21 +647,85 @@ template <typename T>
 static ReachArgs<T> reach_args(const Shape& sh, const Reach& r, const LayerTable& chan, const T* Q,
                                const T* Kc, const T* Vc, const T* Kd, const T* Vd,
                                const int32_t* ctx_len, T* O, float* lse) {
+  LayerTable lord{};  // consumers sorted by channel, stable
+  for (int c = 0, n = 0; c < kMaxLayers && n < sh.L; ++c)
+    for (int l = 0; l < sh.L; ++l)
+      if (chan.v[l] == c) lord.v[n++] = l;
   return ReachArgs<T>{Q, Kc, Vc, Kd, Vd, (const T*)r.Kp, (const T*)r.Vp, ctx_len, O, lse, sh.B,
                       sh.T_new, sh.L, sh.Hq, sh.Hkv, sh.S_cap, r.P, r.P_cap, r.window, r.sinks,
-                      sh.mask_paper, sh.gs, sh.gq, sh.ctx_hi, kLog2e / sqrtf((float)sh.d), chan};
+                      sh.mask_paper, 0, sh.gs, sh.gq, sh.ctx_hi, kLog2e / sqrtf((float)sh.d), chan,
+                      lord};
+}
+
+template <int DH, bool PRE, bool LSE>
+static void reach_dma(ReachArgs<bf16> a, const Shape& sh, uint32_t* queue, hipStream_t s) {
+  using P = PfDma<1, DH>;
+  a.n_qtiles = (sh.T_new + P::BQ - 1) / P::BQ;
+  const long tiles = (long)a.n_qtiles * sh.Hq * sh.B * sh.L, resident = (long)device_cus() * P::WPE;
+  if (tiles <= resident) {
+    hipLaunchKernelGGL((reach_dma_kernel<DH, PRE, LSE>), dim3((unsigned)tiles), dim3(P::NT), 0, s, a,
+                       (uint32_t*)nullptr);
+    return;
+  }
+  hipLaunchKernelGGL(reach_queue_kernel, dim3(1), dim3(kQueueWords), 0, s, queue);
+  hipLaunchKernelGGL((reach_dma_kernel<DH, PRE, LSE>), dim3((unsigned)resident), dim3(P::NT), 0, s, a,
+                     queue);
+}
+
+template <typename T, int DH, bool PRE, bool LSE>
+static void reach_plain(ReachArgs<T> a, const Shape& sh, hipStream_t s) {
+  using C = PrefillCfg<T, DH>;
+  a.n_qtiles = (sh.T_new + C::BQ - 1) / C::BQ;
+  hipLaunchKernelGGL((reach_prefill_kernel<T, DH, PRE, LSE>),
+                     dim3((unsigned)(a.n_qtiles * sh.Hq * sh.B * sh.L)), dim3(C::NT), 0, s, a);
+}
+
+template <typename T, int DH>
+static void prefix_flat(ReachArgs<T> a, int rows, int nlive, hipStream_t s) {
+  using C = PrefillCfg<T, DH>;
+  a.z = (rows + C::BQ - 1) / C::BQ;
+  hipLaunchKernelGGL((reach_prefill_kernel<T, DH, true, false, true>),
+                     dim3((unsigned)(a.z * a.np * a.Hkv * nlive)), dim3(C::NT), 0, s, a);
+}
+
+template <typename T>
+void launch_prefix_rows(const Shape& sh, const Reach& r, const LayerTable& live, int nlive,
+                        const ChannelGroups& cg, int rows, const T* Q, float* part, int nsplit,
+                        int np, int split_len, hipStream_t s) {
+  ReachArgs<T> a = reach_args<T>(sh, r, LayerTable{}, Q, nullptr, nullptr, nullptr, nullptr,
+                                 nullptr, nullptr, nullptr);
+  a.live = live;
+  a.cg = cg;
+  a.part = part;
+  a.np = np;
+  a.nsplit = nsplit;
+  a.split_len = split_len;
+  if constexpr (sizeof(T) == 4) {
+    if (sh.d == 64) return prefix_flat<T, 64>(a, rows, nlive, s);
+  }
+  prefix_flat<T, 32>(a, rows, nlive, s);
+}
+
+template <typename T, bool PRE, bool LSE>
+static void reach_go(const ReachArgs<T>& a, const Shape& sh, uint32_t* queue, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (sh.d == 64) return reach_dma<64, PRE, LSE>(a, sh, queue, s);
+    if (sh.d == 96) return reach_dma<96, PRE, LSE>(a, sh, queue, s);
+  } else {
+    if (sh.d == 64) return reach_plain<T, 64, PRE, LSE>(a, sh, s);
+  }
+  reach_plain<T, 32, PRE, LSE>(a, sh, s);
 }
 
 template <typename T>
 void launch_reach(const Shape& sh, const Reach& r, const LayerTable& chan, const T* Q, const T* Kc,
                   const T* Vc, const T* Kd, const T* Vd, const int32_t* ctx_len, T* O, float* lse,
-                  hipStream_t s) {
+                  void* queue, hipStream_t s) {
   const ReachArgs<T> a = reach_args<T>(sh, r, chan, Q, Kc, Vc, Kd, Vd, ctx_len, O, lse);
-  const long rows = (long)sh.L * sh.N() * sh.Hq;
-  const dim3 grid((unsigned)((rows + 3) / 4));
-  if (sh.d == 32) hipLaunchKernelGGL((reach_rows_kernel<T, 32>), grid, dim3(256), 0, s, a);
-  else if (sh.d == 64) hipLaunchKernelGGL((reach_rows_kernel<T, 64>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((reach_rows_kernel<T, 96>), grid, dim3(256), 0, s, a);
+  uint32_t* q = (uint32_t*)queue;
+  if (lse) reach_go<T, false, true>(a, sh, q, s);
+  else if (r.P > 0) reach_go<T, true, false>(a, sh, q, s);
+  else reach_go<T, false, false>(a, sh, q, s);
 }
 
 template <typename T>
@@ -291,7 +906,10 @@ void launch_reach_backward(const Shape& sh, const Reach& r, const LayerTable& ch
 #define WM_INST(T)                                                                                \
   template void launch_reach<T>(const Shape&, const Reach&, const LayerTable&, const T*,          \
                                 const T*, const T*, const T*, const T*, const int32_t*, T*,       \
-                                float*, hipStream_t);                                             \
+                                float*, void*, hipStream_t);                                      \
+  template void launch_prefix_rows<T>(const Shape&, const Reach&, const LayerTable&, int,         \
+                                      const ChannelGroups&, int, const T*, float*, int, int, int, \
+                                      hipStream_t);                                               \
   template void launch_weigh<T>(const Shape&, const LayerTable&, const ChannelGroups&, const T*,  \
                                 const T*, const int32_t*, const float*, float*, hipStream_t);
 WM_INST(float)
