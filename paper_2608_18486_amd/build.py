@@ -25,6 +25,7 @@ SOURCES = {
     "wm_backward.hip": [],
     "wm_grad.hip": [],
     "wm_reach.hip": [],
+    "wm_reach_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "wm_evict.hip": [],
     "wm_calib.hip": [],
 }

@@ -244,7 +244,7 @@ Layout layout(const wm_dims& dd, int op) {
     Ly.part = take(!decode_path(d) ? wm::kPrefillQueueBytes
                    : op == WM_OP_WINDOW_ATTEND ? wm::decode_window_bytes(make_shape(d))
                                                : wm::decode_partials_bytes(make_shape(d)));
-  if (op == WM_OP_WINDOW_BACKWARD) Ly.part = take(wm::reach_backward_rows_bytes(make_shape(d)));
+  if (op == WM_OP_WINDOW_BACKWARD) Ly.part = take(wm::reach_backward_bytes(make_shape(d)));
   if (op == WM_OP_WEIGH_ATTEND) {
     Ly.lse = take((size_t)d.L * N * d.Hq * 4);
     if (decode_path(d)) Ly.scores = take(wm::decode_scores_bytes(make_shape(d)));

@@ -789,6 +789,30 @@ size_t attend_backward_rows_bytes(const Shape& sh) {
          sizeof(float);
 }
 
+size_t dummy_backward_bytes(const Shape& sh) {
+  return 2ul * sh.k * sh.Hkv * dummy_chunks(sh) * sh.d * sizeof(float);
+}
+
+void launch_dummy_backward(const Shape& sh, const ChannelGroups& groups, const bf16* Q,
+                           const bf16* dO, float* pd, float* dsd, float* part, float* dKd,
+                           float* dVd, hipStream_t s) {
+  BwdArgs a{};
+  a.Q = Q, a.dO = dO, a.pd = pd, a.dsd = dsd, a.dKd = dKd, a.dVd = dVd;
+  a.B = sh.B, a.T = sh.T_new, a.L = sh.L, a.Hq = sh.Hq, a.Hkv = sh.Hkv;
+  a.mask_paper = sh.mask_paper, a.scale = 1.0f / sqrtf((float)sh.d);
+  a.grp = groups, a.dchunks = dummy_chunks(sh);
+  const dim3 gp(sh.k * sh.Hkv * a.dchunks), gs(sh.k * sh.Hkv);
+  if (sh.d == 64) {
+    hipLaunchKernelGGL(attend_bwd_dummy_part_kernel<64>, gp, dim3(4 * 64), 0, s, a, part);
+    hipLaunchKernelGGL(attend_bwd_dummy_sum_kernel<64>, gs, dim3(4 * 64), 0, s, a,
+                       (const float*)part);
+  } else {
+    hipLaunchKernelGGL(attend_bwd_dummy_part_kernel<96>, gp, dim3(4 * 96), 0, s, a, part);
+    hipLaunchKernelGGL(attend_bwd_dummy_sum_kernel<96>, gs, dim3(4 * 96), 0, s, a,
+                       (const float*)part);
+  }
+}
+
 void launch_attend_backward(const Shape& sh, const LayerTable& chan_map,
                             const ChannelGroups& groups, const bf16* Q, const bf16* Kc,
                             const bf16* Vc, const bf16* Kd, const bf16* Vd, const bf16* O,

@@ -171,6 +171,12 @@ void launch_attend_backward(const Shape& sh, const LayerTable& chan_map,
                             float* dVc, float* dKd, float* dVd, float* rows, hipStream_t s,
                             bool accumulate = false);
 
+// The dummy's gradients alone, from its weight pd and dS dsd of every row (wm_backward.hip).
+size_t dummy_backward_bytes(const Shape& sh);
+void launch_dummy_backward(const Shape& sh, const ChannelGroups& groups, const bf16* Q,
+                           const bf16* dO, float* pd, float* dsd, float* part, float* dKd,
+                           float* dVd, hipStream_t s);
+
 // compute units of the current device (cached per device)
 int device_cus();
 
@@ -321,12 +327,12 @@ template <typename T>
 void launch_weigh(const Shape& sh, const LayerTable& chan, const ChannelGroups& cg, const T* Q,
                   const T* Kc, const int32_t* ctx_len, const float* lse, float* weight,
                   hipStream_t s);
-size_t reach_backward_rows_bytes(const Shape& sh);
+size_t reach_backward_bytes(const Shape& sh);
 void launch_reach_backward(const Shape& sh, const Reach& r, const LayerTable& chan,
                            const ChannelGroups& cg, const bf16* Q, const bf16* Kc, const bf16* Vc,
                            const bf16* Kd, const bf16* Vd, const bf16* O, const bf16* dO,
                            const int32_t* ctx_len, float* dQ, float* dKc, float* dVc, float* dKd,
-                           float* dVd, float* rows, hipStream_t s);
+                           float* dVd, float* ws, hipStream_t s);
 size_t evict_index_bytes(const Shape& sh);
 void launch_evict(const Shape& sh, const int32_t* ctx_len, int keep, int first, int recent,
                   const float* weight, const void* Kc, const void* Vc, int S_out,
