@@ -618,29 +618,95 @@ __global__ __launch_bounds__(64 * kPrefillWaves) void reach_prefill_kernel(Reach
   if (LSE && h == 0) a.lse[(((long)l * a.B + b) * a.Hq + hq) * a.T_new + qi] = m + __log2f(lt);
 }
 
-// weight[c][b][kvh][s] += sum of exp2(score - lse) over the rows that read the slot: a wave per
-// slot, its lanes over the rows.
+// ---------------------------------------------------------------- weights of longer calls
+// weight[c][b][kvh][s] += the sum over the rows that read the slot of exp2(score - lse). A workgroup
+// takes 32 CT slots of one slice, whose K rows stay in registers, and its four waves cut the rows
+// (32 at a time: a consumer's head's query block): S^T = K Q^T puts one row and 16 slots in a lane,
+// so a step adds 16 exponentials per slot tile to the lane's sums, and the rows meet across lanes
+// and waves once, at the end, in a fixed order. Query fragments come straight from memory: the
+// waves of a CU read the same few blocks (L1 and L2), each for CT slot tiles.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void reach_weigh_kernel(ReachArgs<T> a, ChannelGroups cg,
                                                           float* weight) {
-  const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int kvh = blockIdx.y % a.Hkv, b = blockIdx.y / a.Hkv % a.B, c = blockIdx.y / a.Hkv / a.B;
-  const int p0 = ctx_at(a.ctx_len, b, a.ctx_hi) + a.gq + (a.mask_paper ? 0 : 1);
-  if (s >= min(p0 + a.gs * (a.T_new - 1), a.S_cap)) return;
-  const int G = a.Hq / a.Hkv, n = (cg.offsets[c + 1] - cg.offsets[c]) * G * a.T_new;
-  const T* kr = a.Kc + ((((long)c * a.B + b) * a.Hkv + kvh) * a.S_cap + s) * DH;
-  float w = 0.f;
-  for (int x = lane; x < n; x += 64) {
-    const int i = x % a.T_new, hq = kvh * G + x / a.T_new % G;
-    const int l = cg.members[cg.offsets[c] + x / a.T_new / G];
-    if (s >= p0 + a.gs * i) continue;
-    const long rid = (((long)l * a.B + b) * a.Hq + hq) * a.T_new + i;
-    float sc = 0.f;
-    for (int e = 0; e < DH; ++e) sc += to_f32(a.Q[rid * DH + e]) * a.scale_log2 * to_f32(kr[e]);
-    w += fast_exp2(sc - a.lse[rid]);
+  constexpr int NKS = DH / 16, CT = 2;
+  __shared__ float s_w[4][32 * CT];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int slice = blockIdx.y, kvh = slice % a.Hkv, b = slice / a.Hkv % a.B, c = slice / a.Hkv / a.B;
+  const int p0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq +
+                 (a.mask_paper ? 0 : 1);  // row i reads slots below p0 + gs i
+  const int kend = min(p0 + a.gs * (a.T_new - 1), a.S_cap);
+  const int sb = 32 * CT * blockIdx.x, G = a.Hq / a.Hkv;
+  const int nh = (cg.offsets[c + 1] - cg.offsets[c]) * G;
+  if (sb >= kend || nh == 0) return;
+  const float cl2 = a.scale_log2;
+  const long cbase = ((long)slice * a.S_cap) * DH;
+  const auto kview = make_view(a.Kc + cbase, (uint32_t)kend * DH * sizeof(T));
+  frag_t<T> kf[CT][NKS];
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+      kf[t][ks] = buf_frag<T>(kview, (uint32_t)((sb + 32 * t + r) * DH + 16 * ks + 8 * h) *
+                                         (uint32_t)sizeof(T));
+  f32x16 acc[CT];
+#pragma unroll
+  for (int t = 0; t < CT; ++t) acc[t] = zero16();
+  // the first row that reads slot sb, rounded down to a block; steps go head by head
+  const int i_num = sb - p0, qb0 = (i_num < 0 ? 0 : i_num / a.gs + 1) / 32;
+  const int nqb = (a.T_new + 31) / 32 - qb0, nst = nh * nqb;
+  frag_t<T> qn[NKS];
+  float lse_n = 0.f;
+  int qi_n = 0;
+  auto fetch = [&](int st) {
+    const int x = st / nqb, l = cg.members[cg.offsets[c] + x / G];
+    const long row0 = (((long)l * a.B + b) * a.Hq + kvh * G + x % G) * a.T_new;
+    qi_n = 32 * (qb0 + st % nqb) + r;
+    const auto qview = make_view(a.Q + row0 * DH, (uint32_t)a.T_new * DH * (uint32_t)sizeof(T));
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+      qn[ks] = buf_frag<T>(qview, (uint32_t)(qi_n * DH + 16 * ks + 8 * h) * (uint32_t)sizeof(T));
+    lse_n = qi_n < a.T_new ? a.lse[row0 + qi_n] : 0.f;
+  };
+  if (w < nst) fetch(w);
+  for (int st = w; st < nst; st += 4) {
+    frag_t<T> qf[NKS];
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) qf[ks] = qn[ks];
+    const float nl = -lse_n;
+    const int qi = qi_n;
+    if (st + 4 < nst) fetch(st + 4);
+    const int lim = qi < a.T_new ? p0 + a.gs * qi : 0;  // (rows past the last read nothing)
+    const int q0 = 32 * (qb0 + st % nqb);
+    const bool all = q0 + 32 <= a.T_new && p0 + a.gs * q0 >= sb + 32 * CT;
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      f32x16 sc = zero16();
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) sc = mma32(sc, kf[t][ks], qf[ks]);
+      if (!all) {
+        const int at = sb + 32 * t + 4 * h;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) sc[q] = at + 8 * (q >> 2) + (q & 3) < lim ? sc[q] : kHidden;
+      }
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[t][q] += fast_exp2(fmaf(sc[q], cl2, nl));
+    }
   }
-  w = wave_sum(w);
-  if (lane == 0 && n > 0) weight[(((long)c * a.B + b) * a.Hkv + kvh) * a.S_cap + s] += w;
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      float v = acc[t][q];
+#pragma unroll
+      for (int x = 1; x < 32; x <<= 1) v += __shfl_xor(v, x, 64);
+      if (r == 0) s_w[w][32 * t + 8 * (q >> 2) + 4 * h + (q & 3)] = v;
+    }
+  __syncthreads();
+  if (tid < 32 * CT && sb + tid < kend) {
+    float* dst = weight + (long)slice * a.S_cap + sb + tid;
+    *dst += (s_w[0][tid] + s_w[1][tid]) + (s_w[2][tid] + s_w[3][tid]);
+  }
 }
 
 template <typename T>
@@ -736,10 +802,17 @@ void launch_weigh(const Shape& sh, const LayerTable& chan, const ChannelGroups& 
   const ReachArgs<T> a = reach_args<T>(sh, r, chan, Q, Kc, nullptr, nullptr, nullptr, ctx_len,
                                        nullptr, const_cast<float*>(lse));
   const long most = (long)sh.ctx_max + sh.span();
-  const dim3 grid((unsigned)((most + 3) / 4), (unsigned)(sh.k * sh.B * sh.Hkv));
-  if (sh.d == 32) hipLaunchKernelGGL((reach_weigh_kernel<T, 32>), grid, dim3(256), 0, s, a, cg, weight);
-  else if (sh.d == 64) hipLaunchKernelGGL((reach_weigh_kernel<T, 64>), grid, dim3(256), 0, s, a, cg, weight);
-  else hipLaunchKernelGGL((reach_weigh_kernel<T, 96>), grid, dim3(256), 0, s, a, cg, weight);
+  const dim3 grid((unsigned)((most + 63) / 64), (unsigned)(sh.k * sh.B * sh.Hkv));
+  if constexpr (sizeof(T) == 2) {
+    if (sh.d == 96) {
+      hipLaunchKernelGGL((reach_weigh_kernel<T, 96>), grid, dim3(256), 0, s, a, cg, weight);
+      return;
+    }
+  }
+  if (sh.d == 64)
+    hipLaunchKernelGGL((reach_weigh_kernel<T, 64>), grid, dim3(256), 0, s, a, cg, weight);
+  else
+    hipLaunchKernelGGL((reach_weigh_kernel<T, 32>), grid, dim3(256), 0, s, a, cg, weight);
 }
 
 #define WM_INST(T)                                                                                \
