@@ -414,9 +414,9 @@ def _want(name, t, shape, dtype):
     """The tensor's pointer, once its shape and type are what the call reads or writes."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+    if t.shape != shape or t.dtype != dtype:
         raise ValueError("%s must be %s of shape %s, got %s of shape %s" %
-                         (name, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+                         (name, dtype, shape, t.dtype, tuple(t.shape)))
     return _ptr(t)
 
 

@@ -8,17 +8,19 @@
 // Angles: turns = (j - s) theta^(-2m/d) / 2 pi and its fraction in fp64 (a position of 10^5 has
 // 10^4 turns, whose fraction fp32 would leave with 3 digits), sine and cosine in fp32.
 #include <algorithm>
+#include <cmath>
 
 #include "wm_device.hpp"
 #include "wm_internal.hpp"
 
 namespace wm {
 
-// Ascending order of the weights as unsigned integers; NaN below everything, -0 as +0.
+// Ascending order of the weights as unsigned integers in [1, 2^32 - 2]; NaN below everything, -0
+// as +0.
 __device__ __forceinline__ uint32_t weight_key(float w) {
-  if (!(w == w)) return 0u;
   const uint32_t u = __float_as_uint(w + 0.0f);
-  return u >> 31 ? ~u : u | 0x80000000u;
+  const uint32_t k = u >> 31 ? ~u : u | 0x80000000u;
+  return w == w ? k : 1u;
 }
 
 struct EvictArgs {
@@ -31,25 +33,33 @@ struct EvictArgs {
   int B, Hkv, S_cap, S_out, ctx_max, keep, first, recent, idx_ld;
 };
 
-// One workgroup per (channel, sequence, KV head): the slots it keeps. The M = keep - first -
-// recent heaviest of the candidates [first, n - recent) are those with a key above the M-th
-// largest, t, and the lowest ones at t: t is found digit by digit (8 bits at a time, from the
-// top) with a histogram of the candidates that share the digits found so far; then one pass in
-// slot order writes the kept slots by their running count.
-constexpr int kSelThreads = 1024;
+// One workgroup per (channel, sequence, KV head): the slots it keeps, the `keep` largest keys and
+// of equal ones the lowest slots (the first and the recent slots get the largest key of all). The
+// keep-th largest key, t, is found digit by digit (11, 11 and 10 bits from the top): a histogram in
+// LDS of the keys that share the digits found so far, whose running sum from the largest bin down
+// every thread takes part in. Then one pass in slot order writes the slots above t, and as many at t
+// as are missing, by their running count. The weights are read once: the first 1024 R slots' keys
+// stay in registers (a wave owns 64 R neighbouring slots, so its running count needs the other
+// waves' totals only); slots past them are read again for every digit. What bounds it is the issue
+// of instructions: two bits at a time by ballots, 16 rounds of 24 compares a wave, took 114 us at
+// 1536 slices of up to 8191 slots and 12 at 36 of 900; this way 51 and 8; histograms of 8 bits
+// scanned by one thread 155 and 38.
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+template <int R>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t s_prefix, s_left;
-  __shared__ int s_above[kSelThreads / 64], s_tie[kSelThreads / 64];
+  constexpr int kBins = 2 * kSelThreads;
+  __shared__ uint32_t s_hist[kBins], s_found[2];
+  __shared__ int s_above[kSelWaves], s_tie[kSelWaves];
   const int slice = blockIdx.x, b = slice / a.Hkv % a.B;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int n = ctx_at(a.ctx_len, b, a.ctx_max);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_max));
   const float* wt = a.weight + (long)slice * a.S_cap;
   int32_t* idx = a.idx + (long)slice * a.idx_ld;
   int32_t* kept = a.kept ? a.kept + (long)slice * a.keep : nullptr;
   float* wo = a.weight_out + (long)slice * a.S_out;
   const int nk = min(n, a.keep);
-  if (slice / a.Hkv < a.B && slice % a.Hkv == 0 && tid == 0) a.ctx_out[b] = nk;
+  if (slice < a.B * a.Hkv && slice % a.Hkv == 0 && tid == 0) a.ctx_out[b] = nk;
   for (int j = nk + tid; j < a.S_out; j += kSelThreads) wo[j] = 0.f;
   if (kept)
     for (int j = nk + tid; j < a.keep; j += kSelThreads) kept[j] = -1;
@@ -61,69 +71,131 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(EvictArgs a) 
     }
     return;
   }
-  const int lo = a.first, hi = n - a.recent;  // candidates
-  const int M = a.keep - a.first - a.recent;  // 0 <= M < hi - lo
-  uint32_t prefix = 0, left = (uint32_t)M;  // digits found; rank still to find among them
-  if (M > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
-      __syncthreads();
-      const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-      for (int s = lo + tid; s < hi; s += kSelThreads) {
-        const uint32_t key = weight_key(wt[s]);
-        if ((key & mask) == prefix) atomicAdd(&hist[key >> shift & 255], 1u);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        uint32_t rank = left;
-        int digit = 255;
-        while (digit > 0 && hist[digit] < rank) rank -= hist[digit--];
-        s_prefix = prefix | (uint32_t)digit << shift;
-        s_left = rank;
-      }
-      __syncthreads();
-      prefix = s_prefix;
-      left = s_left;
+  const int lo = a.first, hi = n - a.recent;  // slots in between are chosen by weight
+  constexpr int RD = kSelThreads * R;         // slots per round of the registers
+  const bool more = n > RD;
+  auto slot = [&](int rd, int j) { return rd + (w * R + j) * 64 + lane; };
+  auto load = [&](int s) { return s < n ? wt[s] : 0.f; };
+  auto key_of = [&](int s, float x) {  // 0 past the last slot: below every threshold
+    const uint32_t k = s >= lo && s < hi ? weight_key(x) : ~0u;
+    return s < n ? k : 0u;
+  };
+  uint32_t key[R];
+  float wv[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) wv[j] = load(slot(0, j));
+#pragma unroll
+  for (int j = 0; j < R; ++j) key[j] = key_of(slot(0, j), wv[j]);
+  uint32_t t = 0, rank = (uint32_t)a.keep;  // digits found; rank among the keys that share them
+  int done = 0;                             // bits found
+  for (int pass = 0; pass < 3; ++pass) {
+    const int bits = pass < 2 ? 11 : 10, shift = 32 - done - bits;
+    s_hist[2 * tid] = s_hist[2 * tid + 1] = 0;
+    __syncthreads();
+    auto add = [&](uint32_t k) {
+      if (done == 0 || k >> (32 - done) == t >> (32 - done))
+        atomicAdd(&s_hist[k >> shift & ((1u << bits) - 1)], 1u);
+    };
+    if (64 * R * w < n) {  // (a wave past the last slot has nothing to count)
+#pragma unroll
+      for (int j = 0; j < R; ++j) add(key[j]);
     }
+    if (more)
+      for (int rd = RD; rd < n; rd += RD)
+        for (int j = 0; j < R; ++j) {
+          const int s = slot(rd, j);
+          add(key_of(s, load(s)));
+        }
+    __syncthreads();
+    // this thread's two bins, the largest ones first: thread 0 holds the last two of 2048
+    const int bin = kBins - 2 - 2 * tid;
+    const uint32_t h1 = s_hist[bin + 1], h0 = s_hist[bin];
+    uint32_t run = h1 + h0;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      const uint32_t v = __shfl_up(run, x, 64);
+      run += lane >= x ? v : 0;
+    }
+    if (lane == 63) s_above[w] = (int)run;
+    __syncthreads();
+    uint32_t before = 0;  // keys in larger bins
+    for (int v = 0; v < w; ++v) before += (uint32_t)s_above[v];
+    before += run - h1 - h0;
+    if (before < rank && before + h1 >= rank) s_found[0] = bin + 1, s_found[1] = rank - before;
+    else if (before + h1 < rank && before + h1 + h0 >= rank)
+      s_found[0] = bin, s_found[1] = rank - before - h1;
+    __syncthreads();
+    t |= s_found[0] << shift;
+    rank = s_found[1];
+    done += bits;
   }
-  // prefix: the M-th largest key; `left` of the candidates at it are kept, the lowest ones
-  int at = 0, ties = 0;  // kept so far, candidates at the threshold so far
-  for (int s0 = 0; s0 < n; s0 += kSelThreads) {
-    const int s = s0 + tid;
-    bool always = false, above = false, tie = false;
-    float wv = 0.f;
-    if (s < n) {
-      wv = wt[s];
-      always = s < lo || s >= hi;
-      const uint32_t key = weight_key(wv);
-      above = !always && M > 0 && key > prefix;
-      tie = !always && M > 0 && key == prefix;
-    }
-    const uint64_t bt = __ballot(tie);
-    if (lane == 0) s_tie[w] = __popcll(bt);
+  t = __builtin_amdgcn_readfirstlane(t);
+  auto exchange = [&](int na, int nt) {  // this wave's counts, everyone's in s_above, s_tie
+    if (lane == 0) s_above[w] = na, s_tie[w] = nt;
     __syncthreads();
-    int tb = ties, tall = 0;
-    for (int k = 0; k < kSelThreads / 64; ++k) {
-      if (k < w) tb += s_tie[k];
-      tall += s_tie[k];
-    }
-    const int tr = tb + __popcll(bt & ((1ull << lane) - 1));  // this tie's rank
-    const bool take = always || above || (tie && tr < (int)left);
-    const uint64_t bk = __ballot(take);
-    if (lane == 0) s_above[w] = __popcll(bk);
+  };
+  auto tally = [&](uint32_t k, int& na, int& nt) {
+    na += __popcll(__builtin_amdgcn_ballot_w64(k > t));
+    nt += __popcll(__builtin_amdgcn_ballot_w64(k == t));
+  };
+  int left = a.keep;  // slots at t to take: what the ones above t leave
+  if (more) {
+    int na = 0, nt = 0;
+    for (int rd = RD; rd < n; rd += RD)
+      for (int j = 0; j < R; ++j) {
+        const int s = slot(rd, j);
+        tally(key_of(s, load(s)), na, nt);
+      }
+    exchange(na, 0);
+    for (int v = 0; v < kSelWaves; ++v) left -= s_above[v];
     __syncthreads();
-    int kb = at, kall = 0;
-    for (int k = 0; k < kSelThreads / 64; ++k) {
-      if (k < w) kb += s_above[k];
-      kall += s_above[k];
+  }
+  int at = 0, ties = 0;  // kept, and slots at t, in the rounds before
+  for (int rd = 0; rd < n; rd += RD) {
+    if (rd > 0) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        wv[j] = load(slot(rd, j));
+        key[j] = key_of(slot(rd, j), wv[j]);
+      }
     }
-    if (take) {
-      const int j = kb + __popcll(bk & ((1ull << lane) - 1));
-      idx[j] = s;
-      if (kept) kept[j] = s;
-      wo[j] = wv;
+    int na = 0, nt = 0;
+#pragma unroll
+    for (int j = 0; j < R; ++j) tally(key[j], na, nt);
+    exchange(na, nt);
+    // before this wave, and in all (lane v holds wave v's counts)
+    int ab = lane < w ? s_above[lane % kSelWaves] : 0, tb = lane < w ? s_tie[lane % kSelWaves] : 0;
+    int aall = lane < kSelWaves ? s_above[lane % kSelWaves] : 0;
+    int tall = lane < kSelWaves ? s_tie[lane % kSelWaves] : 0;
+#pragma unroll
+    for (int x = 1; x < kSelWaves; x <<= 1) {
+      ab += __shfl_xor(ab, x, 64), tb += __shfl_xor(tb, x, 64);
+      aall += __shfl_xor(aall, x, 64), tall += __shfl_xor(tall, x, 64);
     }
-    at += kall;
+    ab = __builtin_amdgcn_readfirstlane(ab);
+    tb = ties + __builtin_amdgcn_readfirstlane(tb);
+    aall = __builtin_amdgcn_readfirstlane(aall);
+    tall = __builtin_amdgcn_readfirstlane(tall);
+    if (rd == 0) left -= aall;
+    // kept before this wave: the rounds before, the waves' above, and the ties taken of theirs
+    int kb = at + ab + min(tb, left) - min(ties, left);
+    const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const int s = slot(rd, j);
+      const uint64_t bt = __builtin_amdgcn_ballot_w64(key[j] == t);
+      const bool take = key[j] > t || (key[j] == t && tb + __popcll(bt & below) < left);
+      const uint64_t bk = __builtin_amdgcn_ballot_w64(take);
+      if (take) {
+        const int o = kb + __popcll(bk & below);
+        idx[o] = s;
+        if (kept) kept[o] = s;
+        wo[o] = wv[j];
+      }
+      kb += __popcll(bk);
+      tb += __popcll(bt);
+    }
+    at += aall + min(ties + tall, left) - min(ties, left);
     ties += tall;
     __syncthreads();
   }
@@ -137,7 +209,7 @@ struct MoveArgs {
   int B, Hkv, S_cap, S_out, ctx_max, keep, idx_ld;
   int b0, nb;          // sequences b0 .. b0 + nb - 1 of the source
   int shift;           // added to the destination's position (idx null)
-  double theta;
+  double log2_theta;
 };
 
 // Rows [0, n) of every destination slice: a thread moves 8 elements of the key's first half,
@@ -147,7 +219,7 @@ __global__ __launch_bounds__(256) void move_rows_kernel(MoveArgs a) {
   constexpr int H = DH / 2, C = H / 8;  // threads per row
   __shared__ double turn[H];            // turns per position
   for (int m = threadIdx.x; m < H; m += 256)
-    turn[m] = pow(a.theta, -2.0 * (double)m / (double)DH) * 0.15915494309189533577;
+    turn[m] = exp2(a.log2_theta * (-2.0 * (double)m / (double)DH)) * 0.15915494309189533577;
   __syncthreads();
   const int slice = blockIdx.y;  // destination (channel, sequence, KV head)
   const int h = slice % a.Hkv, b = slice / a.Hkv % a.nb, c = slice / (a.Hkv * a.nb);
@@ -202,12 +274,18 @@ void launch_evict(const Shape& sh, const int32_t* ctx_len, int keep, int first, 
   const int ld = std::max(sh.ctx_max, 1);
   const EvictArgs e{ctx_len, weight, idx, kept, weight_out, ctx_out, sh.B, sh.Hkv, sh.S_cap,
                     S_out, sh.ctx_max, keep, first, recent, ld};
-  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)(sh.k * sh.B * sh.Hkv)),
-                     dim3(kSelThreads), 0, s, e);
+  // keys in registers: up to 1024 slots in one of them, 8192 in 8, else up to 32768 in 32
+  const dim3 slices((unsigned)(sh.k * sh.B * sh.Hkv)), blk(kSelThreads);
+  if (sh.ctx_max <= kSelThreads)
+    hipLaunchKernelGGL(evict_select_kernel<1>, slices, blk, 0, s, e);
+  else if (sh.ctx_max <= 8 * kSelThreads)
+    hipLaunchKernelGGL(evict_select_kernel<8>, slices, blk, 0, s, e);
+  else
+    hipLaunchKernelGGL(evict_select_kernel<32>, slices, blk, 0, s, e);
   const int most = std::min(keep, sh.ctx_max);
   if (most == 0) return;
   const MoveArgs m{Kc, Vc, Ko, Vo, idx, ctx_len, sh.B, sh.Hkv, sh.S_cap, S_out, sh.ctx_max, most,
-                   ld, 0, sh.B, 0, (double)sh.rope_theta};
+                   ld, 0, sh.B, 0, log2((double)sh.rope_theta)};
   if (bf) move_rows<bf16>(m, sh.k, sh.d, s);
   else move_rows<float>(m, sh.k, sh.d, s);
 }
@@ -215,7 +293,7 @@ void launch_evict(const Shape& sh, const int32_t* ctx_len, int keep, int first, 
 void launch_prefix_share(const Shape& sh, const void* Kc, const void* Vc, int seq, int len,
                          int P_cap, void* Kp, void* Vp, bool bf, hipStream_t s) {
   const MoveArgs m{Kc, Vc, Kp, Vp, nullptr, nullptr, sh.B, sh.Hkv, sh.S_cap, P_cap, 0, len, 0,
-                   seq, 1, -len, (double)sh.rope_theta};
+                   seq, 1, -len, log2((double)sh.rope_theta)};
   if (bf) move_rows<bf16>(m, sh.k, sh.d, s);
   else move_rows<float>(m, sh.k, sh.d, s);
 }
