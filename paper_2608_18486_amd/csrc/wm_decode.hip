@@ -8,7 +8,7 @@
 
 #include "wm_device.hpp"
 #include "wm_frag.hpp"
-#include "wm_internal.hpp"
+#include "wm_prefill.hpp"
 
 namespace wm {
 
@@ -156,19 +156,17 @@ __device__ __forceinline__ void lds_dma16_stream(uint32_t lds_addr, uint32_t vof
                : "memory", "m0");
 }
 
-template <int DH, int NW, bool DOC, bool ONCE, bool WIN = false, bool SCORES = false>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(3)))
-void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
+// (split, slice y and row tile z of the grid; smem: NW rings)
+template <int DH, int NW, bool DOC, bool ONCE, bool WIN, bool SCORES>
+__device__ __forceinline__ void decode_block(const DecodeArgs<bf16>& a, const int split, int y,
+                                             const int z, char* smem) {
   using C = DecMfma<DH, NW>;
-  __shared__ __align__(16) char smem[C::NW * C::RING];
-  const int split = blockIdx.x;
-  int y = blockIdx.y;
   const int kvh = y % a.Hkv;
   y /= a.Hkv;
   const int b = y % a.B, ci = y / a.B, c = a.live.v[ci];
   const int off = a.cg.offsets[ci], nmem = a.cg.offsets[ci + 1] - off;
   const int grp = a.Hq / a.Hkv;
-  const int G = nmem * grp * a.T_new, g0 = 32 * blockIdx.z;
+  const int G = nmem * grp * a.T_new, g0 = 32 * z;
   if (g0 >= G) return;
   const int pos0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq;
   const int gs = a.gs, incl = a.mask_paper ? 0 : 1;
@@ -358,6 +356,13 @@ void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
       dst[DH + 1] = lw;
     }
   }
+}
+
+template <int DH, int NW, bool DOC, bool ONCE, bool WIN = false, bool SCORES = false>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(3)))
+void attend_decode_mfma_kernel(DecodeArgs<bf16> a) {
+  __shared__ __align__(16) char smem[NW * DecMfma<DH, NW>::RING];
+  decode_block<DH, NW, DOC, ONCE, WIN, SCORES>(a, blockIdx.x, blockIdx.y, blockIdx.z, smem);
 }
 
 // ---------------------------------------------- decode on the VALU (fp32, head dim 32)
@@ -619,19 +624,36 @@ __global__ __launch_bounds__(256) void decode_weigh_kernel(DecodeArgs<T> a, floa
 // ------------------------------------------------- the shared prefix, few new tokens
 // A prefix slot is read by every sequence, so the rows of one (channel, KV head) are those of the
 // whole batch (consumers x grouped heads x new tokens x sequences), each seeing every slot:
-// products of 32 RT rows per wave against blocks of 32 slots, where a sequence's own cache meets
-// only its own few rows. As in the decode kernel above, a wave walks blocks of its own through a
-// ring of two in LDS; every block it has read serves its RT row tiles, and the row tiles of a
-// split run next to each other on one XCD, whose L2 holds the split's slots for all of them.
+// products of up to 128 rows against blocks of 32 slots, where a sequence's own cache meets only
+// its own few rows. A workgroup's two waves share the blocks they read: either each has RT tiles of
+// 32 rows of its own (RW = 2), wave 0 copying K and wave 1 V into a ring of three blocks, or, where a
+// slice has 32 rows at most, both take the same rows and every second block (RW = 1, a ring of two
+// pairs). Scores and weights as in decode_block, the weights in 24 bits.
+// The workgroups of a prefix's splits and those of the sequences' own caches (decode_block) form
+// one grid: the former are bound by their products and exponentials, the latter by the stream of the
+// cache, and a CU holds some of each at a time. (64 sequences, 24 layers of 16 heads of 64, 4096 + 300
+// slots: 222 us; in two launches, the prefix by waves with rings of their own, 256.)
 struct PrefixSpan {
-  int P, P_cap, nsplit, split_len, z;  // z: workgroups of 32 RT rows per (slice, split)
+  const bf16 *Kp, *Vp;
+  int P, P_cap, nsplit, split_len, z;  // z: workgroups of rows per (slice, split)
+  int blocks;                          // workgroups of the prefix, ahead of the caches'
+  int own, slices;                     // splits and slices of the sequences' own caches
 };
-template <int DH, int NW, int RT>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(DH == 64 ? 3 : 2)))
-void attend_prefix_mfma_kernel(DecodeArgs<bf16> a, PrefixSpan px) {
-  using C = DecMfma<DH, NW>;
-  __shared__ __align__(16) char smem[C::NW * C::RING];
-  const int tile = xcd_tile(blockIdx.x, (int)gridDim.x);
+template <int DH, int RW, int RT> struct PrefixCfg {
+  static constexpr int NW = 2, SW = NW / RW, NS = RW == 2 ? 3 : 2;  // SW: waves that cut the slots
+  static constexpr int NKS = DH / 16, NDT = DH / 32, ROW_BYTES = 2 * DH, CPR = ROW_BYTES / 16;
+  static constexpr int BLK = 32 * ROW_BYTES, NI = BLK / 1024;
+  static constexpr int STAGE = SW * 2 * BLK;     // per block: K then V
+  static constexpr int PER = SW * 2 * NI / NW;   // copy instructions of a wave per stage
+  static constexpr int ROWS = 32 * RT * RW;      // rows of a workgroup
+  static constexpr int OLD = DH + 4, MERGE = 32 * OLD * 4 + 256;  // a tile's state in LDS
+  static constexpr int SMEM = NS * STAGE > NW * MERGE ? NS * STAGE : NW * MERGE;
+};
+template <int DH, int RW, int RT>
+__device__ __forceinline__ void prefix_block(const DecodeArgs<bf16>& a, const PrefixSpan& px,
+                                             char* smem) {
+  using C = PrefixCfg<DH, RW, RT>;
+  const int tile = xcd_tile(blockIdx.x, px.blocks);
   const int zt = tile % px.z;
   int y = tile / px.z;
   const int split = y % px.nsplit;
@@ -639,110 +661,151 @@ void attend_prefix_mfma_kernel(DecodeArgs<bf16> a, PrefixSpan px) {
   const int kvh = y % a.Hkv, ci = y / a.Hkv, c = a.live.v[ci];
   const int off = a.cg.offsets[ci], nmem = a.cg.offsets[ci + 1] - off;
   const int grp = a.Hq / a.Hkv, per_b = nmem * grp * a.T_new;
-  const int G = per_b * a.B, g0 = 32 * RT * zt;
+  const int G = per_b * a.B, g0 = C::ROWS * zt;
   if (g0 >= G) return;
   const int s0 = split * px.split_len, s1 = min(s0 + px.split_len, px.P);
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = RW == 2 ? w : 0, sw = RW == 2 ? 0 : w;  // this wave's row tiles, its blocks
   const float cl2 = a.scale_log2;
-  auto row_of = [&](int g) {
-    const int b = g / per_b, x = g % per_b, i = x % a.T_new, gq = x / a.T_new % grp;
-    const int l = a.cg.members[off + x / (a.T_new * grp)];
-    return (((long)l * a.B + b) * a.Hq + kvh * grp + gq) * a.T_new + i;
-  };
-  bf16x8 qf[RT][C::NKS];
+  int row[RT];  // this lane's rows [l][b][hq][i] (both halves of the wave alike), -1 past the last
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const bool ok = g0 + 32 * t + r < G;
-    const long rowid = ok ? row_of(g0 + 32 * t + r) : 0;
-#pragma unroll
-    for (int ks = 0; ks < C::NKS; ++ks)
-      qf[t][ks] = ok ? ld_frag<bf16>(a.Q + rowid * DH + 16 * ks + 8 * h) : zero_frag<bf16>();
+    const int g = g0 + 32 * (RT * rw + t) + r, b = g / per_b, x = g % per_b, gl = x / a.T_new;
+    const int l = a.cg.members[off + gl / grp];
+    row[t] = g < G ? ((l * a.B + b) * a.Hq + kvh * grp + gl % grp) * a.T_new + x % a.T_new : -1;
   }
-  const int nblk = s1 > s0 ? (s1 - s0 + C::BKV - 1) / C::BKV : 0;
-  const int nw = (nblk - w + C::NW - 1) / C::NW;
-  const long cbase = ((long)c * a.Hkv + kvh) * (long)px.P_cap * DH;
-  const auto kview = make_view(a.Kc + cbase, (uint32_t)px.P * C::ROW_BYTES);
-  const auto vview = make_view(a.Vc + cbase, (uint32_t)px.P * C::ROW_BYTES);
   uint32_t coff[C::NI];
 #pragma unroll
   for (int n = 0; n < C::NI; ++n) {
     const int ch = 64 * n + lane, row = ch / C::CPR;
     coff[n] = (uint32_t)row * C::ROW_BYTES + 16u * (uint32_t)((ch % C::CPR) ^ pf_swz<DH>(row));
   }
-  char* ring = smem + w * C::RING;
-  const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
-  auto issue = [&](int j, int st) {
-    const uint32_t base =
-        j < nw ? (uint32_t)(s0 + C::BKV * (w + C::NW * j)) * C::ROW_BYTES : kOffOob;
+  const int nblk = (s1 - s0 + 31) / 32, nit = (nblk + C::SW - 1) / C::SW;
+  const long cbase = ((long)c * a.Hkv + kvh) * (long)px.P_cap * DH;
+  const auto kview = make_view(px.Kp + cbase, (uint32_t)px.P * C::ROW_BYTES);
+  const auto vview = make_view(px.Vp + cbase, (uint32_t)px.P * C::ROW_BYTES);
+  const uint32_t smem_at = (uint32_t)(uintptr_t)smem;
+  // step it into stage st: wave w copies instructions w PER .. of its blocks' K and V (past the
+  // last step zeros, so that the copies in flight are the same number at every wait)
+  auto issue = [&](int it, int st) {
 #pragma unroll
-    for (int n = 0; n < 2 * C::NI; ++n)
-      lds_dma16(__builtin_amdgcn_readfirstlane(ring_at + st * C::STAGE + 1024 * n),
-                base + coff[n % C::NI], n < C::NI ? kview : vview);
+    for (int i = 0; i < C::PER; ++i) {
+      const bool v = RW == 2 ? w == 1 : i >= C::NI;
+      const int at = s0 + 32 * (it * C::SW + sw);
+      const uint32_t base = it < nit ? (uint32_t)at * C::ROW_BYTES : kOffOob;
+      lds_dma16(__builtin_amdgcn_readfirstlane(smem_at + st * C::STAGE + 1024 * (w * C::PER + i)),
+                base + coff[i % C::NI], v ? vview : kview);
+    }
   };
+  issue(0, 0);
+  if (C::NS == 3) issue(1, 1);
+  bf16x8 qf[RT][C::NKS];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+#pragma unroll
+    for (int ks = 0; ks < C::NKS; ++ks)
+      qf[t][ks] = row[t] >= 0 ? ld_frag<bf16>(a.Q + (long)row[t] * DH + 16 * ks + 8 * h)
+                           : zero_frag<bf16>();
+  }
   float m[RT], lsum[RT];
   f32x16 o[RT][C::NDT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    m[t] = kNegBig;
+    m[t] = kNoRef;
     lsum[t] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < C::NDT; ++dt) o[t][dt] = zero16();
   }
   const PfLane<DH> lo = pf_lane<DH>(lane);
-  issue(0, 0);
-  int j = 0, st = 0;
-  do {
+  for (int it = 0, st = 0; it < nit; ++it) {
+    wait_copies<(C::NS - 2) * C::PER>();
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
-    issue(j + 1, st ^ 1);
-    wait_copies<2 * C::NI>();
-    const uint32_t kh = st * C::STAGE, vh = kh + C::BLK;
-    const int at = s0 + C::BKV * (w + C::NW * j);
+    __syncthreads();  // step it has landed, and the stage of step it - 1 is free
+    issue(it + C::NS - 1, st == 0 ? C::NS - 1 : st - 1);
+    const uint32_t kh = st * C::STAGE + sw * 2 * C::BLK, vh = kh + C::BLK;
+    const int at = s0 + 32 * (it * C::SW + sw);
+    // scores of both row tiles, then their weights against the rows' references (log2 units),
+    // which move only where a weight would pass 2^12 (or at a row's first slots)
+    f32x16 p[RT];
+    auto scores = [&]() {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) p[t] = zero16();
+#pragma unroll
+      for (int ks = 0; ks < C::NKS; ++ks) {
+        const bf16x8 kf = pf_ldk<DH>(smem, lo, kh, ks);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) p[t] = mma32(p[t], kf, qf[t][ks]);
+      }
+      if (__builtin_expect(at + 32 > s1, 0)) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int q = 0; q < 16; ++q)
+            p[t][q] = at + 4 * h + 8 * (q >> 2) + (q & 3) >= s1 ? kNegBig : p[t][q];
+      }
+    };
+    float ps[RT];
+    bool far = false;
+    scores();
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      f32x16 sc = zero16();
 #pragma unroll
-      for (int ks = 0; ks < C::NKS; ++ks) sc = mma32(sc, pf_ldk<DH>(ring, lo, kh, ks), qf[t][ks]);
-      if (__builtin_expect(at + C::BKV > s1, 0)) {
+      for (int q = 0; q < 16; ++q) p[t][q] = fast_exp2(fmaf(p[t][q], cl2, -m[t]));
+      ps[t] = sum16(p[t]);
+      far |= !(ps[t] <= kGrowSum) || m[t] == kNoRef;
+    }
+    if (__builtin_expect(__any(far), 0)) {
+      scores();
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
-          sc[q] = at + 4 * h + 8 * (q >> 2) + (q & 3) >= s1 ? kNegBig : sc[q];
-      }
-      float mx = sc[0];
+      for (int t = 0; t < RT; ++t) {
+        float mx = p[t][0];
 #pragma unroll
-      for (int q = 1; q < 16; ++q) mx = fmaxf(mx, sc[q]);
-      mx = halves_max(mx);
-      if (__builtin_expect(__any(mx > m[t]), 0)) {
-        const float mn = fmaxf(m[t], mx), al = fast_exp2((m[t] - mn) * cl2);
+        for (int q = 1; q < 16; ++q) mx = fmaxf(mx, p[t][q]);
+        mx = halves_max(mx);
+        const bool none = !(mx > 0.5f * kNegBig);  // every slot hidden: the reference stays
+        const float grow = none ? 0.f : ref_growth(fmaf(mx, cl2, -m[t]), m[t]);
+        const float al = ref_rescale(grow, m[t]);
+        m[t] += grow;
         lsum[t] *= al;
 #pragma unroll
-        for (int dt = 0; dt < C::NDT; ++dt) {
-          asm volatile("" : "+v"(o[t][dt]));  // (keeps the products out of the common path)
-          o[t][dt] *= al;
-        }
-        m[t] = mn;
+        for (int dt = 0; dt < C::NDT; ++dt) o[t][dt] *= al;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) p[t][q] = fast_exp2(fmaf(p[t][q], cl2, -m[t]));
+        ps[t] = sum16(p[t]);
       }
-      const float mc = m[t] > 0.5f * kNegBig ? m[t] * cl2 : 0.f;
-      f32x16 p;
-#pragma unroll
-      for (int q = 0; q < 16; ++q) p[q] = fast_exp2(fmaf(sc[q], cl2, -mc));
-      lsum[t] += sum16(p);
-      bf16x8 pw[3][2];
-      cut24(p, pw);
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-        for (int dt = 0; dt < C::NDT; ++dt) {
-          const bf16x8 vf = pf_ldv<DH>(ring, lo, vh, hf, dt);
-#pragma unroll
-          for (int u = 0; u < 3; ++u) o[t][dt] = mma32(o[t][dt], vf, pw[u][hf]);
-        }
     }
-    st ^= 1;
-  } while (++j < nw);
+    // weights in two rounded bf16 parts, 17 bits: off by 2^-18 of each term, where the result is
+    // rounded to 2^-9 of itself (with a third part, and the exact maximum at every block, the prefix
+    // alone took 87 us instead of 66)
+    bf16x8 pw[RT][2][2];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      lsum[t] += ps[t];
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const bf16 hi = (bf16)p[t][q];
+        pw[t][0][q >> 3][q & 7] = hi;
+        pw[t][1][q >> 3][q & 7] = (bf16)(p[t][q] - (float)hi);
+      }
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int dt = 0; dt < C::NDT; ++dt) {
+        const bf16x8 vf = pf_ldv<DH>(smem, lo, vh, hf, dt);
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) o[t][dt] = mma32(o[t][dt], vf, pw[t][u][hf]);
+      }
+    st = st + 1 == C::NS ? 0 : st + 1;
+  }
   wait_copies<0>();  // no copy may land in the staging below, or after the block ends
-  // merge the waves' states, a row tile at a time
-  float* so = (float*)ring;
+  asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+  __syncthreads();
+  // a tile's states through LDS: a wave's own rows (RW = 2), or the two waves' merged
+  float* so = (float*)(smem + w * C::MERGE);
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const float lt = halves_sum(lsum[t]);
@@ -756,26 +819,22 @@ void attend_prefix_mfma_kernel(DecodeArgs<bf16> a, PrefixSpan px) {
         *(f32x4*)(so + r * C::OLD + 32 * dt + 8 * g + 4 * h) = v;
       }
     if (h == 0) {
-      so[32 * C::OLD + 2 * r] = m[t];
+      so[32 * C::OLD + 2 * r] = m[t] / cl2;  // in score units, as decode_block's
       so[32 * C::OLD + 2 * r + 1] = lt;
     }
     __syncthreads();
-    const int ng = min(32, G - g0 - 32 * t);
-    for (int e = tid; e < ng * DH; e += C::NT) {
-      const int gi = e / DH, dd = e - gi * DH;
-      float M = kNegBig;
-#pragma unroll
-      for (int ww = 0; ww < C::NW; ++ww)
-        M = fmaxf(M, ((const float*)(smem + ww * C::RING))[32 * C::OLD + 2 * gi]);
-      float lw = 0.f, ow = 0.f;
-#pragma unroll
-      for (int ww = 0; ww < C::NW; ++ww) {
-        const float* sw = (const float*)(smem + ww * C::RING);
-        const float al = fast_exp2((sw[32 * C::OLD + 2 * gi] - M) * cl2);
-        lw += sw[32 * C::OLD + 2 * gi + 1] * al;
-        ow += sw[gi * C::OLD + dd] * al;
+    for (int e = RW == 2 ? lane : tid; e < 32 * DH; e += RW == 2 ? 64 : 128) {
+      const int gi = e / DH, dd = e - gi * DH, to = __shfl(row[t], gi, 64);
+      if (to < 0) continue;
+      const float* s_a = RW == 2 ? so : (const float*)smem;
+      float M = s_a[32 * C::OLD + 2 * gi], lw = s_a[32 * C::OLD + 2 * gi + 1];
+      float ow = s_a[gi * C::OLD + dd];
+      if constexpr (RW == 1) {
+        const float* s_b = (const float*)(smem + C::MERGE);
+        merge_state(M, lw, &ow, s_b[32 * C::OLD + 2 * gi], s_b[32 * C::OLD + 2 * gi + 1],
+                    s_b + gi * C::OLD + dd, 1, cl2);
       }
-      float* dst = a.part + (row_of(g0 + 32 * t + gi) * a.nsplit + split) * (DH + 2);
+      float* dst = a.part + ((long)to * a.nsplit + split) * (DH + 2);
       dst[dd] = ow;
       if (dd == 0) {
         dst[DH] = M;
@@ -784,6 +843,19 @@ void attend_prefix_mfma_kernel(DecodeArgs<bf16> a, PrefixSpan px) {
     }
     __syncthreads();
   }
+}
+
+template <int DH, int RW, int RT, bool ONCE>
+__global__ __launch_bounds__(128) __attribute__((amdgpu_waves_per_eu(2)))
+void attend_shared_mfma_kernel(DecodeArgs<bf16> a, PrefixSpan px) {
+  constexpr int kOwn = 2 * DecMfma<DH, 2>::RING, kPre = PrefixCfg<DH, RW, RT>::SMEM;
+  __shared__ __align__(16) char smem[kOwn > kPre ? kOwn : kPre];
+  if ((int)blockIdx.x < px.blocks) {
+    prefix_block<DH, RW, RT>(a, px, smem);
+    return;
+  }
+  const int x = blockIdx.x - px.blocks, y = x / px.own;
+  decode_block<DH, 2, false, ONCE, false, false>(a, x % px.own, y % px.slices, y / px.slices, smem);
 }
 
 template <typename T, int DH, bool WIN, bool SCORES>
@@ -820,8 +892,14 @@ constexpr long kDecodeMfmaBlocks = 512;
 // Cache (256 MB) can keep next to the rest of a step stays plain.
 constexpr long kDecodeStreamBytes = 128L << 20;
 
+// The matrix-core kernel's grid of the sequences' own slots: splits (a.split_len and a.nsplit are
+// set), row tiles, and whether the slots are read once.
+struct DecodePlan {
+  int own, z;
+  bool once;
+};
 template <int DH>
-static void decode_mfma(DecodeArgs<bf16>& a, int G, int nlive, const Shape& sh, hipStream_t s) {
+static DecodePlan decode_plan(DecodeArgs<bf16>& a, int G, int nlive, const Shape& sh) {
   const int z = std::max(1, (G + 31) / 32);
   const long slices = (long)nlive * sh.B * sh.Hkv * z, kend = (long)sh.ctx_max + sh.span();
   int len = kSplitMax;
@@ -829,10 +907,18 @@ static void decode_mfma(DecodeArgs<bf16>& a, int G, int nlive, const Shape& sh, 
   a.split_len = len;  // at least decode_split_len, so the partials fit their workspace
   const int own = std::max(1, (int)((kend + len - 1) / len));
   a.nsplit = a.split0 + own;
-  const dim3 grid(own, sh.Hkv * sh.B * nlive, z);
   // a cache read once by one row tile, and larger (all channels: layer by layer, the other
   // layers' calls read theirs in between) than the caches keep from call to call
   const bool once = z == 1 && 4L * sh.k * sh.B * sh.Hkv * kend * DH >= kDecodeStreamBytes;
+  return {own, z, once};
+}
+
+template <int DH>
+static void decode_mfma(DecodeArgs<bf16>& a, int G, int nlive, const Shape& sh, hipStream_t s) {
+  const auto [own, z, once] = decode_plan<DH>(a, G, nlive, sh);
+  const long slices = (long)nlive * sh.B * sh.Hkv * z, kend = (long)sh.ctx_max + sh.span();
+  const int len = a.split_len;
+  const dim3 grid(own, sh.Hkv * sh.B * nlive, z);
   // Waves per workgroup: 2, which leaves a CU's LDS to five workgroups (three at head dim
   // 96); 1 where a workgroup's walk is at most 128 slots (four blocks); 4 where the workgroups
   // fit the CUs all at once with four (one per CU at head dim 96, two at 64), and at head dim
@@ -965,44 +1051,52 @@ void launch_weigh_decode(const Shape& sh, const LayerTable& chan_map, const Chan
 }
 
 // -- shared prefix
-// Row tiles of 32 per wave: two where a slice has more than 32 rows (they share every block read).
-static int prefix_tiles(const Shape& sh) {
-  const long rows = (long)sh.L * sh.B * (sh.Hq / sh.Hkv) * sh.T_new / sh.k;
-  return rows > 32 ? 2 : 1;
-}
-// Slots per split of the prefix and its splits, by the dims alone (they size the workspace): as
-// in the decode plan, halved until two workgroups per CU.
-static int prefix_split_len(const Shape& sh, int P) {
-  const long rows = (long)sh.L * sh.B * (sh.Hq / sh.Hkv) * sh.T_new / sh.k;
-  const int per = 32 * prefix_tiles(sh);
-  const long slices = (long)sh.k * sh.Hkv * std::max(1L, (rows + per - 1) / per);
-  int len = kSplitMax;
-  while (len > kSplitMin && slices * ((P + len - 1) / len) < kDecodeMfmaBlocks) len /= 2;
-  return len;
-}
-static int prefix_splits(const Shape& sh, int P) {
-  const int len = prefix_split_len(sh, P);
-  return (P + len - 1) / len;
+// The prefix's grid by the dims alone (it sizes the workspace): row tiles per workgroup, splits.
+struct PrefixPlan {
+  int rw, rt, z, nsplit, split_len;
+};
+static PrefixPlan prefix_plan(const Shape& sh, int P) {
+  const long rows = (long)sh.L * sh.B * (sh.Hq / sh.Hkv) * sh.T_new / sh.k;  // of a slice, evenly
+  PrefixPlan p{rows > 32 ? 2 : 1, rows > 64 ? 2 : 1, 1, 1, std::max(P, 1)};
+  p.z = (int)std::max(1L, (rows + 32 * p.rt * p.rw - 1) / (32 * p.rt * p.rw));
+  // Splits until there are three workgroups for two CUs, of 256 slots or more: the sequences' own
+  // workgroups take the places left, and every split is a state per row to write and read. (us a
+  // call with 2 / 4 / 8 splits: 64 sequences over 4096 + 300 slots, 192 slices of 128 rows 222 /
+  // 232 / 248; over 4096 + 100, 24 slices of 256 rows of 96 111 / 72 / 64.)
+  const long base = (long)sh.k * sh.Hkv * p.z, cus = device_cus();
+  const long most = std::max(1, (P + kSplitMin - 1) / kSplitMin);
+  p.nsplit = (int)std::min(most, std::max(1L, (3 * cus / 2 + base - 1) / base));
+  p.split_len = ((P + p.nsplit - 1) / p.nsplit + 63) / 64 * 64;
+  p.nsplit = std::max(1, (P + p.split_len - 1) / std::max(p.split_len, 1));
+  return p;
 }
 size_t decode_shared_bytes(const Shape& sh, int P) {
   const size_t rows = (size_t)sh.L * sh.B * sh.Hq * sh.T_new;
-  return rows * (decode_splits(sh) + prefix_splits(sh, P)) * (sh.d + 2) * sizeof(float);
+  return rows * (decode_splits(sh) + (P > 0 ? prefix_plan(sh, P).nsplit : 0)) * (sh.d + 2) *
+         sizeof(float);
 }
 
-template <int DH, int NW, int RT>
-static void prefix_go(const DecodeArgs<bf16>& a, const PrefixSpan& px, int nlive, hipStream_t s) {
-  const dim3 grid((unsigned)(px.z * px.nsplit * a.Hkv * nlive));
-  hipLaunchKernelGGL((attend_prefix_mfma_kernel<DH, NW, RT>), grid, dim3(64 * NW), 0, s, a, px);
-}
 template <int DH>
-static void prefix_states(const DecodeArgs<bf16>& a, PrefixSpan px, int G, int nlive,
-                          const Shape& sh, hipStream_t s) {
-  const int rt = prefix_tiles(sh);
-  px.z = (G * sh.B + 32 * rt - 1) / (32 * rt);
-  // four waves where the workgroups leave CUs to themselves, as in the decode plan
-  const bool four = (long)px.z * px.nsplit * a.Hkv * nlive <= device_cus();
-  if (rt == 2) four ? prefix_go<DH, 4, 2>(a, px, nlive, s) : prefix_go<DH, 2, 2>(a, px, nlive, s);
-  else four ? prefix_go<DH, 4, 1>(a, px, nlive, s) : prefix_go<DH, 2, 1>(a, px, nlive, s);
+static void shared_mfma(DecodeArgs<bf16>& a, const Reach& r, const PrefixPlan& p, int G, int nlive,
+                        const Shape& sh, hipStream_t s) {
+  const DecodePlan d = decode_plan<DH>(a, G, nlive, sh);
+  const int rows = 32 * p.rt * p.rw, z = (G * sh.B + rows - 1) / rows;
+  const PrefixSpan px{(const bf16*)r.Kp, (const bf16*)r.Vp, r.P, r.P_cap, p.nsplit, p.split_len, z,
+                      z * p.nsplit * sh.Hkv * nlive, d.own, sh.Hkv * sh.B * nlive};
+  const dim3 grid((unsigned)(px.blocks + (long)d.own * px.slices * d.z));
+#define WM_SHARED_GO(RW, RT)                                                                     \
+  do {                                                                                           \
+    if (d.once)                                                                                  \
+      hipLaunchKernelGGL((attend_shared_mfma_kernel<DH, RW, RT, true>), grid, dim3(128), 0, s, a,  \
+                         px);                                                                    \
+    else                                                                                         \
+      hipLaunchKernelGGL((attend_shared_mfma_kernel<DH, RW, RT, false>), grid, dim3(128), 0, s, a, \
+                         px);                                                                    \
+  } while (0)
+  if (p.rt == 2) WM_SHARED_GO(2, 2);
+  else if (p.rw == 2) WM_SHARED_GO(2, 1);
+  else WM_SHARED_GO(1, 1);
+#undef WM_SHARED_GO
 }
 
 template <typename T>
@@ -1014,22 +1108,19 @@ void launch_shared_decode(const Shape& sh, const Reach& r, const LayerTable& cha
   int nlive, G;
   DecodeArgs<T> a = decode_args<T>(sh, chan_map, cg, Q, Kc, Vc, Kd, Vd, ctx_len, nullptr, partials,
                                    O, &nlive, &G);
-  PrefixSpan px{r.P, r.P_cap, prefix_splits(sh, r.P), prefix_split_len(sh, r.P), 1};
-  a.split0 = r.P > 0 ? px.nsplit : 0;
-  decode_states<T>(a, sh, G, nlive, s);
-  if (r.P > 0) {
-    DecodeArgs<T> ap = a;
-    ap.Kc = (const T*)r.Kp;
-    ap.Vc = (const T*)r.Vp;
-    bool done = false;
-    if constexpr (sizeof(T) == 2) {
-      done = sh.d != 32;
-      if (sh.d == 96) prefix_states<96>(ap, px, G, nlive, sh, s);
-      else if (sh.d == 64) prefix_states<64>(ap, px, G, nlive, sh, s);
-    }
-    if (!done)
-      launch_prefix_rows<T>(sh, r, a.live, nlive, a.cg, G * sh.B, Q, partials, a.nsplit, px.nsplit,
-                            px.split_len, s);
+  const PrefixPlan p = prefix_plan(sh, r.P);
+  a.split0 = r.P > 0 ? p.nsplit : 0;
+  bool done = false;
+  if constexpr (sizeof(T) == 2) {
+    done = sh.d != 32 && r.P > 0;
+    if (done) sh.d == 96 ? shared_mfma<96>(a, r, p, G, nlive, sh, s)
+                         : shared_mfma<64>(a, r, p, G, nlive, sh, s);
+  }
+  if (!done) {
+    decode_states<T>(a, sh, G, nlive, s);
+    if (r.P > 0)
+      launch_prefix_rows<T>(sh, r, a.live, nlive, a.cg, G * sh.B, Q, partials, a.nsplit, p.nsplit,
+                            p.split_len, s);
   }
   decode_combine<T>(a, sh.d, s);
 }
