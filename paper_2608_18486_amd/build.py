@@ -24,7 +24,7 @@ SOURCES = {
     "wm_few.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "wm_backward.hip": [],
     "wm_grad.hip": [],
-    "wm_reach.hip": [],
+    "wm_reach.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "wm_reach_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "wm_evict.hip": [],
     "wm_calib.hip": [],

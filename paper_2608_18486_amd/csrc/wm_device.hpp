@@ -138,6 +138,15 @@ __device__ __forceinline__ void lds_dma16(uint32_t lds_addr, uint32_t voff,
                : "memory", "m0");
 }
 
+// The same with 4 bytes per lane.
+__device__ __forceinline__ void lds_dma4(uint32_t lds_addr, uint32_t voff,
+                                         __amdgpu_buffer_rsrc_t rsrc) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :
+               : "s"(lds_addr), "v"(voff), "s"(rsrc)
+               : "memory", "m0");
+}
+
 // s_waitcnt vmcnt(n) (expcnt and lgkmcnt left alone), n < 64: bits 3..0 and 15..14
 template <int N> __device__ __forceinline__ void wait_vmcnt() {
   static_assert(N >= 0 && N < 64, "vmcnt range");

@@ -632,11 +632,13 @@ __global__ __launch_bounds__(256) void reach_weigh_kernel(ReachArgs<T> a, Channe
   __shared__ float s_w[4][32 * CT];
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int slice = blockIdx.y, kvh = slice % a.Hkv, b = slice / a.Hkv % a.B, c = slice / a.Hkv / a.B;
+  // the slot tiles of a slice, which read the same queries, on one XCD
+  const int tile = xcd_tile(blockIdx.x, (int)gridDim.x), slice = tile / a.n_qtiles;
+  const int kvh = slice % a.Hkv, b = slice / a.Hkv % a.B, c = slice / a.Hkv / a.B;
   const int p0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq +
                  (a.mask_paper ? 0 : 1);  // row i reads slots below p0 + gs i
   const int kend = min(p0 + a.gs * (a.T_new - 1), a.S_cap);
-  const int sb = 32 * CT * blockIdx.x, G = a.Hq / a.Hkv;
+  const int sb = 32 * CT * (tile % a.n_qtiles), G = a.Hq / a.Hkv;
   const int nh = (cg.offsets[c + 1] - cg.offsets[c]) * G;
   if (sb >= kend || nh == 0) return;
   const float cl2 = a.scale_log2;
@@ -700,6 +702,141 @@ __global__ __launch_bounds__(256) void reach_weigh_kernel(ReachArgs<T> a, Channe
       float v = acc[t][q];
 #pragma unroll
       for (int x = 1; x < 32; x <<= 1) v += __shfl_xor(v, x, 64);
+      if (r == 0) s_w[w][32 * t + 8 * (q >> 2) + 4 * h + (q & 3)] = v;
+    }
+  __syncthreads();
+  if (tid < 32 * CT && sb + tid < kend) {
+    float* dst = weight + (long)slice * a.S_cap + sb + tid;
+    *dst += (s_w[0][tid] + s_w[1][tid]) + (s_w[2][tid] + s_w[3][tid]);
+  }
+}
+
+// bf16 at head dims 64 and 96: the same with the query blocks copied into a ring of three in LDS per
+// wave (fragments loaded from memory touch 32 lines an instruction, which the CU's L1 looks up one
+// by one), two score sets in turn, and the slot tiles of a slice on one XCD, whose L2 then serves
+// its queries to all of them. 2 x 1023 tokens, 16 layers of 6/3 heads of 96: 62 us; with the tiles
+// over the XCDs 81, from memory 77.
+template <int DH>
+__global__ __launch_bounds__(256) void reach_weigh_dma_kernel(ReachArgs<bf16> a, ChannelGroups cg,
+                                                              float* weight) {
+  constexpr int NKS = DH / 16, CT = 2, NS = 3, ROW = 2 * DH, CPR = ROW / 16;
+  constexpr int BLK = 32 * ROW, NI = BLK / 1024, STAGE = BLK + 256, RING = NS * STAGE;
+  __shared__ __align__(16) char smem[4 * RING];
+  __shared__ float s_w[4][32 * CT];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // the slot tiles of a slice, which read the same queries, on one XCD
+  const int tile = xcd_tile(blockIdx.x, (int)gridDim.x), slice = tile / a.n_qtiles;
+  const int kvh = slice % a.Hkv, b = slice / a.Hkv % a.B, c = slice / a.Hkv / a.B;
+  const int p0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq +
+                 (a.mask_paper ? 0 : 1);
+  const int kend = min(p0 + a.gs * (a.T_new - 1), a.S_cap);
+  const int sb = 32 * CT * (tile % a.n_qtiles), G = a.Hq / a.Hkv;
+  const int nh = (cg.offsets[c + 1] - cg.offsets[c]) * G;
+  if (sb >= kend || nh == 0) return;
+  const float cl2 = a.scale_log2;
+  const auto kview = make_view(a.Kc + (long)slice * a.S_cap * DH, (uint32_t)kend * ROW);
+  bf16x8 kf[CT][NKS];
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks)
+      kf[t][ks] = buf_frag<bf16>(kview, (uint32_t)(sb + 32 * t + r) * ROW + (16 * ks + 8 * h) * 2u);
+  f32x16 acc[CT];
+#pragma unroll
+  for (int t = 0; t < CT; ++t) acc[t] = zero16();
+  const int i_num = sb - p0, qb0 = (i_num < 0 ? 0 : i_num / a.gs + 1) / 32;
+  const int nqb = (a.T_new + 31) / 32 - qb0, nst = nh * nqb;
+  const int mine = nst > w ? (nst - w + 3) / 4 : 0;  // steps w, w + 4, ... are this wave's
+  char* ring = smem + w * RING;
+  const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
+  uint32_t coff[NI];
+#pragma unroll
+  for (int n = 0; n < NI; ++n) {
+    const int ch = 64 * n + lane, row = ch / CPR;
+    coff[n] = (uint32_t)row * ROW + 16u * (uint32_t)((ch % CPR) ^ pf_swz<DH>(row));
+  }
+  // the next step to copy: head x (of the slice's consumers' heads), query block qb
+  int x = 0, qb = w;
+  auto issue = [&](int st) {  // its rows and their LSE; past the last step zeros
+    if (qb >= nqb) x += qb / nqb, qb %= nqb;
+    const bool ok = x < nh;
+    const int hx = ok ? x : 0, l = cg.members[cg.offsets[c] + hx / G];
+    const long row0 = (((long)l * a.B + b) * a.Hq + kvh * G + hx % G) * a.T_new;
+    const auto qview = make_view(a.Q + row0 * DH, (uint32_t)a.T_new * ROW);
+    const auto lview = make_view(a.lse + row0, (uint32_t)a.T_new * 4u);
+    const uint32_t base = ok ? (uint32_t)(qb0 + qb) * BLK : kOffOob, to = ring_at + st * STAGE;
+#pragma unroll
+    for (int n = 0; n < NI; ++n)
+      lds_dma16(__builtin_amdgcn_readfirstlane(to + 1024 * n), base + coff[n], qview);
+    lds_dma4(__builtin_amdgcn_readfirstlane(to + BLK),
+             ok ? (uint32_t)(32 * (qb0 + qb) + r) * 4u : kOffOob, lview);
+    qb += 4;
+  };
+  const PfLane<DH> lo = pf_lane<DH>(lane);
+  // The scores of step j + 1 are multiplied while the exponentials of step j are taken; two score
+  // sets take turns. When step j starts, step j + 1's copies have landed or are waited for, step
+  // j + 2's are in flight.
+  issue(0);
+  issue(1);
+  int q_at = w, st = 0;  // the next scored step's query block (of nqb per head), its ring stage
+  struct Scored {
+    f32x16 sc[CT];
+    float nl;
+    int q0;
+  } sa, sn;
+  auto score = [&](Scored& s) {
+    if (q_at >= nqb) q_at %= nqb;
+    s.q0 = 32 * (qb0 + q_at);
+    q_at += 4;
+    s.nl = -*(const float*)(ring + st * STAGE + BLK + 4 * r);
+#pragma unroll
+    for (int t = 0; t < CT; ++t) s.sc[t] = zero16();
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      const bf16x8 qf = pf_ldk<DH>(ring, lo, st * STAGE, ks);
+#pragma unroll
+      for (int t = 0; t < CT; ++t) s.sc[t] = mma32(s.sc[t], kf[t][ks], qf);
+    }
+    st = st + 1 == NS ? 0 : st + 1;
+  };
+  auto step = [&](Scored& cur, Scored& nxt) {
+    // steps past the last are scored from zeros and not added
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the stage refilled next is read
+    issue(st + 1 == NS ? 0 : st + 1);
+    wait_copies<NI + 1>();
+    if (cur.q0 + 32 > a.T_new || p0 + a.gs * cur.q0 < sb + 32 * CT) {
+      const int qi = cur.q0 + r;
+      const int lim = qi < a.T_new ? p0 + a.gs * qi : 0;  // (rows past the last read nothing)
+#pragma unroll
+      for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          cur.sc[t][q] =
+              sb + 32 * t + 4 * h + 8 * (q >> 2) + (q & 3) < lim ? cur.sc[t][q] : kHidden;
+    }
+    score(nxt);
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[t][q] += fast_exp2(fmaf(cur.sc[t][q], cl2, cur.nl));
+  };
+  if (mine > 0) {
+    wait_copies<NI + 1>();
+    score(sa);
+    for (int j = 0; j < mine; j += 2) {
+      step(sa, sn);
+      if (j + 1 < mine) step(sn, sa);
+    }
+  }
+  wait_copies<0>();  // no copy may land after the workgroup ends
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      float v = acc[t][q];
+#pragma unroll
+      for (int y = 1; y < 32; y <<= 1) v += __shfl_xor(v, y, 64);
       if (r == 0) s_w[w][32 * t + 8 * (q >> 2) + 4 * h + (q & 3)] = v;
     }
   __syncthreads();
@@ -799,20 +936,24 @@ void launch_weigh(const Shape& sh, const LayerTable& chan, const ChannelGroups& 
                   const T* Kc, const int32_t* ctx_len, const float* lse, float* weight,
                   hipStream_t s) {
   const Reach r{};
-  const ReachArgs<T> a = reach_args<T>(sh, r, chan, Q, Kc, nullptr, nullptr, nullptr, ctx_len,
-                                       nullptr, const_cast<float*>(lse));
+  ReachArgs<T> a = reach_args<T>(sh, r, chan, Q, Kc, nullptr, nullptr, nullptr, ctx_len, nullptr,
+                                 const_cast<float*>(lse));
   const long most = (long)sh.ctx_max + sh.span();
-  const dim3 grid((unsigned)((most + 63) / 64), (unsigned)(sh.k * sh.B * sh.Hkv));
+  a.n_qtiles = (int)((most + 63) / 64);  // slot tiles of a slice
+  const dim3 grid((unsigned)((long)a.n_qtiles * sh.k * sh.B * sh.Hkv));
   if constexpr (sizeof(T) == 2) {
-    if (sh.d == 96) {
-      hipLaunchKernelGGL((reach_weigh_kernel<T, 96>), grid, dim3(256), 0, s, a, cg, weight);
+    if (sh.d == 96)
+      hipLaunchKernelGGL(reach_weigh_dma_kernel<96>, grid, dim3(256), 0, s, a, cg, weight);
+    else if (sh.d == 64)
+      hipLaunchKernelGGL(reach_weigh_dma_kernel<64>, grid, dim3(256), 0, s, a, cg, weight);
+    if (sh.d != 32) return;
+  } else {
+    if (sh.d == 64) {
+      hipLaunchKernelGGL((reach_weigh_kernel<T, 64>), grid, dim3(256), 0, s, a, cg, weight);
       return;
     }
   }
-  if (sh.d == 64)
-    hipLaunchKernelGGL((reach_weigh_kernel<T, 64>), grid, dim3(256), 0, s, a, cg, weight);
-  else
-    hipLaunchKernelGGL((reach_weigh_kernel<T, 32>), grid, dim3(256), 0, s, a, cg, weight);
+  hipLaunchKernelGGL((reach_weigh_kernel<T, 32>), grid, dim3(256), 0, s, a, cg, weight);
 }
 
 #define WM_INST(T)                                                                                \
