@@ -382,17 +382,32 @@ __global__ void reach_queue_kernel(uint32_t* queue) { queue[threadIdx.x] = 0u; }
 // ------------------------------------------- fp32, and bf16 at head dim 32
 // The same tiles without the pipeline: 256 rows per workgroup (8 waves of 32), K and V blocks of
 // 64 slots double-buffered in LDS through registers, V transposed for fp32 (whose matrix
-// instructions have no transposing read). fp32 products run on the fp32 matrix cores, an eighth of
-// the bf16 rate, which bounds this form. FLAT: the rows are the batch's rows of one (channel, KV
+// instructions have no transposing read). fp32 products run on the fp32 matrix cores, a sixteenth of
+// the bf16 rate, which bounds this form. Calls of at most 64 rows per head take 4 waves, two for the
+// rows, each pair cutting a block's slots (SW = 2; their states meet in LDS): 5 sequences x 37
+// tokens over 777 + 50 slots, 12 layers of 12 heads of 64, 197 us with 8 waves of which two had
+// rows, 122 so. FLAT: the rows are the batch's rows of one (channel, KV
 // head) side by side, the slots a split of the prefix, the result a partial state per row.
-template <typename T, int DH, bool PRE, bool LSE, bool FLAT = false>
-__global__ __launch_bounds__(64 * kPrefillWaves) void reach_prefill_kernel(ReachArgs<T> a) {
-  using C = PrefillCfg<T, DH>;
-  static_assert(C::QT == 1, "one tile of 32 rows per wave");
+template <typename T, int DH, int SW_> struct ReachCfg {
+  static constexpr int SW = SW_, NW = SW == 2 ? 4 : 8, NT = 64 * NW, RW = NW / SW;
+  static constexpr int BQ = 32 * RW, BKV = 64;
+  typedef PrefillCfg<T, DH> P;
+  static constexpr int LDK = P::LDK, LDV = P::LDV, VS = P::VS, NKS = P::NKS, NDT = P::NDT;
+  static constexpr bool VTR = P::VTR;
+  static constexpr int KIT = P::KIT, VIT = P::VIT;  // fragments (V: or key pairs) of a block
+  static constexpr int KFR = (KIT + NT - 1) / NT, VPT = (VIT + NT - 1) / NT;  // ... per thread
+  static_assert(SW == 1 || RW * 32 * (DH + 2) * 4 <= 2 * BKV * LDK * (int)sizeof(T),
+                "the merge staging fits the K blocks");
+};
+template <typename T, int DH, bool PRE, bool LSE, bool FLAT = false, int SW = 1>
+__global__ __launch_bounds__(SW == 2 ? 256 : 512) void reach_prefill_kernel(ReachArgs<T> a) {
+  using C = ReachCfg<T, DH, SW>;
   __shared__ __align__(16) T Ks[2][C::BKV * C::LDK];
   __shared__ __align__(16) T Vt[2][C::VS];
   const int tile = xcd_tile(blockIdx.x, (int)gridDim.x);
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, h = lane >> 5, r = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
+  // this wave's rows, and (SW = 2) its half of every block
+  const int w = (tid >> 6) % C::RW, phase = (tid >> 6) / C::RW;
   const float cl2 = a.scale_log2;
   int l = 0, b = 0, hq = 0, kvh, c, q0, kend = 0, split = 0, rows = a.T_new;
   int off = 0, lim, wlim0, wlim1, rlo, wlo0, wlo1;
@@ -448,7 +463,7 @@ __global__ __launch_bounds__(64 * kPrefillWaves) void reach_prefill_kernel(Reach
   f32x16 o[C::NDT];
 #pragma unroll
   for (int dt = 0; dt < C::NDT; ++dt) o[dt] = zero16();
-  if (!FLAT && a.mask_paper) {
+  if (!FLAT && a.mask_paper && phase == 0) {
     const T* kd = a.Kd + ((long)c * a.Hkv + kvh) * DH;
     const T* vd = a.Vd + ((long)c * a.Hkv + kvh) * DH;
     float part = 0.f;
@@ -585,12 +600,34 @@ __global__ __launch_bounds__(64 * kPrefillWaves) void reach_prefill_kernel(Reach
     for (int kt = 0; kt < 2; ++kt) {
       const int x0 = k0 + 32 * kt;
       // wave-uniform: some row may read some of the 32 slots
-      if (live && x0 < wlim1 && (x0 + 32 > wlo0 || x0 < sp.first)) half(x0, kt, Ks[buf], Vt[buf]);
+      if (live && (SW == 1 || kt == phase) && x0 < wlim1 && (x0 + 32 > wlo0 || x0 < sp.first)) half(x0, kt, Ks[buf], Vt[buf]);
     }
     stage(buf ^ 1);
     __syncthreads();
   }
-  const float lt = halves_sum(lsum);
+  float lt = halves_sum(lsum);
+  if constexpr (SW == 2) {  // the second half's state joins the first's (every wave is past the loop)
+    float* so = (float*)&Ks[0][0] + w * 32 * (DH + 2) + r * (DH + 2);
+    if (phase == 1) {
+#pragma unroll
+      for (int dt = 0; dt < C::NDT; ++dt)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) so[32 * dt + 8 * (q >> 2) + 4 * h + (q & 3)] = o[dt][q];
+      if (h == 0) so[DH] = m, so[DH + 1] = lt;
+    }
+    __syncthreads();
+    if (phase == 1) return;
+    const float m2 = so[DH], l2 = so[DH + 1];
+    const float M = l2 > 0.f && (m2 > m || !(lt > 0.f)) ? m2 : m;
+    const float f1 = lt > 0.f ? fast_exp2(m - M) : 0.f, f2 = l2 > 0.f ? fast_exp2(m2 - M) : 0.f;
+    lt = lt * f1 + l2 * f2;
+    m = M;
+#pragma unroll
+    for (int dt = 0; dt < C::NDT; ++dt)
+#pragma unroll
+      for (int q = 0; q < 16; ++q)
+        o[dt][q] = o[dt][q] * f1 + so[32 * dt + 8 * (q >> 2) + 4 * h + (q & 3)] * f2;
+  }
   if (qi >= rows) return;
   if constexpr (FLAT) {  // the decode kernels' partial state: o unnormalised, m in score units, l
     float* dst = a.part + (qrow * a.nsplit + split) * (DH + 2);
@@ -875,17 +912,22 @@ static void reach_dma(ReachArgs<bf16> a, const Shape& sh, uint32_t* queue, hipSt
                      queue);
 }
 
-template <typename T, int DH, bool PRE, bool LSE>
-static void reach_plain(ReachArgs<T> a, const Shape& sh, hipStream_t s) {
-  using C = PrefillCfg<T, DH>;
+template <typename T, int DH, bool PRE, bool LSE, int SW>
+static void reach_plain_go(ReachArgs<T> a, const Shape& sh, hipStream_t s) {
+  using C = ReachCfg<T, DH, SW>;
   a.n_qtiles = (sh.T_new + C::BQ - 1) / C::BQ;
-  hipLaunchKernelGGL((reach_prefill_kernel<T, DH, PRE, LSE>),
+  hipLaunchKernelGGL((reach_prefill_kernel<T, DH, PRE, LSE, false, SW>),
                      dim3((unsigned)(a.n_qtiles * sh.Hq * sh.B * sh.L)), dim3(C::NT), 0, s, a);
+}
+template <typename T, int DH, bool PRE, bool LSE>
+static void reach_plain(const ReachArgs<T>& a, const Shape& sh, hipStream_t s) {
+  if (sh.T_new <= ReachCfg<T, DH, 2>::BQ) reach_plain_go<T, DH, PRE, LSE, 2>(a, sh, s);
+  else reach_plain_go<T, DH, PRE, LSE, 1>(a, sh, s);
 }
 
 template <typename T, int DH>
 static void prefix_flat(ReachArgs<T> a, int rows, int nlive, hipStream_t s) {
-  using C = PrefillCfg<T, DH>;
+  using C = ReachCfg<T, DH, 1>;
   a.z = (rows + C::BQ - 1) / C::BQ;
   hipLaunchKernelGGL((reach_prefill_kernel<T, DH, true, false, true>),
                      dim3((unsigned)(a.z * a.np * a.Hkv * nlive)), dim3(C::NT), 0, s, a);
