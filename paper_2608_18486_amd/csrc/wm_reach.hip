@@ -379,6 +379,201 @@ void reach_dma_kernel(ReachArgs<bf16> a, uint32_t* queue) {
 
 __global__ void reach_queue_kernel(uint32_t* queue) { queue[threadIdx.x] = 0u; }
 
+// ------------------------------------------------ bf16, head dims 64 and 96, few rows per head
+// A workgroup takes 32 rows of one head and its four waves cut the compact slots between them, as
+// attend_tile_kernel does (wm_tile.hip): blocks of 32 slots go round the waves, each with a ring
+// of two in LDS of its own, and the waves' states meet in LDS once. A 128-row tile would leave
+// three or two of its four waves without rows, and walk its range as one chain. Slot x of a block
+// is found per row of the block, so first slots and window need not start at a block's edge. Times
+// beside the rule that chooses it.
+template <int DH, bool PRE, bool LSE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void reach_few_kernel(ReachArgs<bf16> a) {
+  constexpr int NW = 4, NKS = DH / 16, NDT = DH / 32, ROW = 2 * DH, CPR = ROW / 16, BKV = 32;
+  constexpr int BLK = BKV * ROW, NI = BLK / 1024, STAGE = 2 * BLK, RING = 2 * STAGE;
+  constexpr int OLD = DH + 4;  // row stride of the merge staging (floats)
+  static_assert(32 * OLD * 4 + 256 <= RING, "the merge staging fits a wave's ring");
+  __shared__ __align__(16) char smem[NW * RING];
+  const int tile = xcd_tile(blockIdx.x, (int)gridDim.x);
+  const int qtile = a.n_qtiles - 1 - tile % a.n_qtiles;
+  const int G = a.Hq / a.Hkv;
+  int y = tile / a.n_qtiles;
+  const int hg = y % G;
+  y /= G;
+  const int li = y % a.L;
+  y /= a.L;
+  const int kvh = y % a.Hkv, b = y / a.Hkv;
+  const int hq = kvh * G + hg, l = a.lord.v[li], c = a.chan.v[l];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int pos0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq;
+  const int incl = a.mask_paper ? 0 : 1, gs = a.gs;
+  const float cl2 = a.scale_log2;
+  const int q0 = qtile * 32, qi = q0 + r, qlast = min(q0 + 32, a.T_new) - 1;
+  const int kend = min(pos0 + gs * qlast + incl, a.S_cap);
+  const ReachSpan sp = reach_span<bf16, PRE>(a, pos0 + gs * q0 + incl, kend);
+  const int off = pos0 + incl + sp.own - sp.skip;
+  const int lim = off + gs * min(qi, a.T_new - 1), wlim0 = off + gs * q0, wlim1 = off + gs * qlast;
+  const int rlo = PRE ? sp.low : lim - sp.low, wlo1 = PRE ? sp.low : wlim1 - sp.low;
+  const int nblk = (sp.n + BKV - 1) / BKV, nw = (nblk - w + NW - 1) / NW;
+
+  const long cbase = (((long)c * a.B + b) * a.Hkv + kvh) * (long)a.S_cap * DH;
+  const auto kview = make_view(a.Kc + cbase, (uint32_t)max(kend, 0) * ROW);
+  const auto vview = make_view(a.Vc + cbase, (uint32_t)max(kend, 0) * ROW);
+  const long pbase = PRE ? ((long)c * a.Hkv + kvh) * (long)a.P_cap * DH : 0;
+  const uint32_t pbytes = PRE ? (uint32_t)a.P * ROW : 0u;
+  const auto kpview = make_view(PRE ? a.Kp + pbase : nullptr, pbytes);
+  const auto vpview = make_view(PRE ? a.Vp + pbase : nullptr, pbytes);
+  uint32_t coff[NI];
+#pragma unroll
+  for (int n = 0; n < NI; ++n) {
+    const int ch = 64 * n + lane, row = ch / CPR;
+    coff[n] = (uint32_t)row * ROW + 16u * (uint32_t)((ch % CPR) ^ pf_swz<DH>(row));
+  }
+  char* ring = smem + w * RING;
+  const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
+  // block j of this wave into stage st (past the wave's last: zeros, so that the copies in flight
+  // are the same number at every wait)
+  auto issue = [&](int j, int st) {
+    const int at = BKV * (w + NW * j);
+    const bool pre = PRE && at < sp.own;
+    const uint32_t base = j < nw ? (uint32_t)(PRE && !pre ? at - sp.own : at) * ROW : kOffOob;
+#pragma unroll
+    for (int n = 0; n < 2 * NI; ++n) {
+      uint32_t o = base + coff[n % NI];
+      if constexpr (!PRE)
+        o += at + (64 * (n % NI) + lane) / CPR >= sp.na ? (uint32_t)sp.skip * ROW : 0u;
+      const uint32_t to = __builtin_amdgcn_readfirstlane(ring_at + st * STAGE + 1024 * n);
+      if constexpr (PRE) lds_dma16(to, o, pre ? (n < NI ? kpview : vpview) : (n < NI ? kview : vview));
+      else lds_dma16(to, o, n < NI ? kview : vview);
+    }
+  };
+
+  bf16x8 qf[NKS];
+  const auto qv = make_view(a.Q + (((long)l * a.B + b) * a.Hq + hq) * (long)a.T_new * DH,
+                            (uint32_t)a.T_new * ROW);
+  const bool dummy = a.mask_paper && w == 0;
+  const long dof = ((long)c * a.Hkv + kvh) * DH;
+  const auto kdv = make_view(dummy ? a.Kd + dof : nullptr, dummy ? ROW : 0u);
+  const auto vdv = make_view(dummy ? a.Vd + dof : nullptr, dummy ? ROW : 0u);
+  float part = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < NKS; ++ks) {
+    const uint32_t col = (uint32_t)(16 * ks + 8 * h) * 2u;
+    qf[ks] = buf_frag<bf16>(qv, qi < a.T_new ? (uint32_t)qi * ROW + col : kOffOob);
+    const bf16x8 kd = buf_frag<bf16>(kdv, col);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part += (float)qf[ks][i] * (float)kd[i];
+  }
+  f32x16 o[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const bf16x4 vd = buf_ld8(vdv, (32 * dt + 8 * g + 4 * h) * 2u);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[dt][4 * g + i] = (float)vd[i];
+    }
+  float m = dummy ? halves_sum(part) * cl2 : kNoRef, lsum = dummy && h == 0 ? 1.f : 0.f;
+
+  const PfLane<DH> lo = pf_lane<DH>(lane);
+  issue(0, 0);
+  int j = 0;
+  do {  // (a wave without a block walks one of zeros, every slot of it hidden)
+    const int st = j & 1;
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the stage refilled next is read
+    issue(j + 1, st ^ 1);
+    wait_copies<2 * NI>();
+    const uint32_t kh = st * STAGE, vh = kh + BLK;
+    const int at = BKV * (w + NW * j);
+    const bool masked = at + BKV > wlim0 || (at < wlo1 && at + BKV > sp.first);
+    auto scores = [&]() {
+      f32x16 s = zero16();
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) s = mma32(s, pf_ldk<DH>(ring, lo, kh, ks), qf[ks]);
+      if (masked) reach_mask(s, at / 32, j < nw ? lim : 0, rlo, j < nw ? sp.first : 0, lane);
+      return s;
+    };
+    f32x16 p = scores();
+#pragma unroll
+    for (int q = 0; q < 16; ++q) p[q] = fast_exp2(fmaf(p[q], cl2, -m));
+    bf16x8 pf[2];
+#pragma unroll
+    for (int q = 0; q < 16; ++q) pf[q >> 3][q & 7] = (bf16)p[q];
+    float ps = LSE ? tree_sum<0, 16>(p) : pf_wsum(pf[0], pf[1]);
+    if (__builtin_expect(__any(!(ps <= kGrowSum) || m == kNoRef), 0)) {
+      p = scores();
+      float mx = p[0];
+#pragma unroll
+      for (int q = 1; q < 16; ++q) mx = fmaxf(mx, p[q]);
+      const float grow = ref_growth(fmaf(halves_max(mx), cl2, -m), m), alpha = ref_rescale(grow, m);
+      m += grow;
+      lsum *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) o[dt] *= alpha;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        p[q] = fast_exp2(fmaf(p[q], cl2, -m));
+        pf[q >> 3][q & 7] = (bf16)p[q];
+      }
+      ps = LSE ? tree_sum<0, 16>(p) : pf_wsum(pf[0], pf[1]);
+    }
+    lsum += ps;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) o[dt] = mma32(o[dt], pf_ldv<DH>(ring, lo, vh, hf, dt), pf[hf]);
+  } while (++j < nw);
+  wait_copies<0>();  // no copy may land in the staging below, or after the block ends
+
+  // merge the waves' states: each writes its rows [r][DH] and (m, l) to its own ring
+  asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+  float* so = (float*)ring;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      f32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = o[dt][4 * g + i];
+      *(f32x4*)(so + r * OLD + 32 * dt + 8 * g + 4 * h) = v;
+    }
+  const float lt = halves_sum(lsum);
+  if (h == 0) {
+    so[32 * OLD + 2 * r] = m;
+    so[32 * OLD + 2 * r + 1] = lt;
+  }
+  __syncthreads();
+  constexpr int C4 = DH / 4;
+  for (int e = tid; e < 32 * C4; e += 64 * NW) {
+    const int row = e / C4, d4 = 4 * (e - row * C4);
+    if (q0 + row >= a.T_new) break;  // rows only grow
+    float M = kNegBig;  // of the waves that saw a slot
+#pragma unroll
+    for (int ww = 0; ww < NW; ++ww) {
+      const float* ml = (const float*)(smem + ww * RING) + 32 * OLD + 2 * row;
+      M = ml[1] > 0.f ? fmaxf(M, ml[0]) : M;
+    }
+    float lw = 0.f, ow[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ww = 0; ww < NW; ++ww) {
+      const float* sw = (const float*)(smem + ww * RING);
+      const float lx = sw[32 * OLD + 2 * row + 1];
+      const float al = lx > 0.f ? fast_exp2(sw[32 * OLD + 2 * row] - M) : 0.f;
+      lw += lx * al;
+      const f32x4 ov = *(const f32x4*)(sw + row * OLD + d4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ow[i] += ov[i] * al;
+    }
+    const float inv = 1.0f / lw;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ow[i] *= inv;
+    store4(a.O + ((((long)l * a.B + b) * a.T_new + q0 + row) * a.Hq + hq) * DH + d4, ow);
+    if (LSE && d4 == 0)
+      a.lse[(((long)l * a.B + b) * a.Hq + hq) * a.T_new + q0 + row] = M + __log2f(lw);
+  }
+}
+
 // ------------------------------------------- fp32, and bf16 at head dim 32
 // The same tiles without the pipeline: 256 rows per workgroup (8 waves of 32), K and V blocks of
 // 64 slots double-buffered in LDS through registers, V transposed for fp32 (whose matrix
@@ -900,6 +1095,17 @@ static ReachArgs<T> reach_args(const Shape& sh, const Reach& r, const LayerTable
 template <int DH, bool PRE, bool LSE>
 static void reach_dma(ReachArgs<bf16> a, const Shape& sh, uint32_t* queue, hipStream_t s) {
   using P = PfDma<1, DH>;
+  // Tiles of 32 rows whose waves cut the slots where a head has no more rows, or up to three of
+  // them for two CUs. us a call, 128-row tiles / these: 16 layers of 6/3 heads of 96, window 1024, one
+  // sequence of 64 / 128 / 256 tokens (192 / 384 / 768 workgroups) 24 / 27 / 29 and 15 / 24 / 36;
+  // 24 layers of 16 heads of 64, window 512, 8 sequences of 16 / 40 tokens 66 / 79 and
+  // 63 / 108; over a prefix of 2000, 16 sequences of 16 / 40 257 / 324 and 224 / 389.
+  const long few = (long)((sh.T_new + 31) / 32) * sh.Hq * sh.B * sh.L;
+  if (sh.T_new <= 32 || 2 * few <= 3l * device_cus()) {
+    a.n_qtiles = (sh.T_new + 31) / 32;
+    hipLaunchKernelGGL((reach_few_kernel<DH, PRE, LSE>), dim3((unsigned)few), dim3(256), 0, s, a);
+    return;
+  }
   a.n_qtiles = (sh.T_new + P::BQ - 1) / P::BQ;
   const long tiles = (long)a.n_qtiles * sh.Hq * sh.B * sh.L, resident = (long)device_cus() * P::WPE;
   if (tiles <= resident) {
