@@ -21,6 +21,7 @@
 #include "wm_device.hpp"
 #include "wm_frag.hpp"
 #include "wm_internal.hpp"
+#include "wm_prefill.hpp"
 
 namespace wm {
 
@@ -37,27 +38,35 @@ struct ReachBwdArgs {
   ChannelGroups grp;
 };
 
-constexpr int kReachBwdWaves = 4;  // waves per workgroup, 32 rows or slots each
+constexpr int kReachBwdWaves = 4;  // waves per workgroup
 constexpr float kHiddenScore = -__builtin_inff();
 
-// Rows row0 .. row0 + ROWS - 1 (row_bytes apart in the view) into the LDS block at lds_base in the
-// fragment readers' chunk order; rows at or past `na` lie `skip` further on, rows at or past
-// nvalid arrive as zeros. Every wave of the NW issues its share; the caller waits (vmcnt).
-template <int DH, int ROWS, int NW>
-__device__ __forceinline__ void reach_copy(uint32_t lds_base, __amdgpu_buffer_rsrc_t view,
-                                           uint32_t row_bytes, int row0, int na, int skip,
-                                           int nvalid, int w, int lane) {
-  constexpr int CPR = DH * 2 / 16, TOT = ROWS * CPR, NI = TOT / (64 * NW);
+// A thread's share of copying ROWS rows (row_bytes apart in memory) into an LDS block in the
+// fragment readers' chunk order: byte offsets of its 16-byte chunks within the block of rows, and
+// their rows. Views end at the last row, so rows past it arrive as zeros.
+template <int DH, int ROWS, int NW> struct ReachCopy {
+  static constexpr int CPR = DH * 2 / 16, TOT = ROWS * CPR, NI = TOT / (64 * NW);
   static_assert(NI * 64 * NW == TOT, "whole instructions per wave");
+  uint32_t off[NI];
+  int row[NI];
+  __device__ __forceinline__ ReachCopy(uint32_t row_bytes, int w, int lane) {
 #pragma unroll
-  for (int n = 0; n < NI; ++n) {
-    const int pos = (NI * w + n) * 64 + lane, row = pos / CPR, cc = pos - row * CPR;
-    const int x = row0 + row, gr = x < na ? x : x + skip;
-    const uint32_t off = x < nvalid ? (uint32_t)gr * row_bytes + 16u * (uint32_t)(cc ^ pf_swz<DH>(row))
-                                    : kOffOob;
-    lds_dma16(__builtin_amdgcn_readfirstlane(lds_base + (NI * w + n) * 1024), off, view);
+    for (int n = 0; n < NI; ++n) {
+      const int pos = (NI * w + n) * 64 + lane, cc = pos % CPR;
+      row[n] = pos / CPR;
+      off[n] = (uint32_t)row[n] * row_bytes + 16u * (uint32_t)(cc ^ pf_swz<DH>(row[n]));
+    }
   }
-}
+  // Rows from byte `base` of the view on into LDS at lds_base (this wave's chunks follow its w);
+  // rows at or past `na` of the block lie `skip` bytes further on.
+  __device__ __forceinline__ void go(uint32_t lds_base, __amdgpu_buffer_rsrc_t view, uint32_t base,
+                                     int w, int na = ROWS, uint32_t skip = 0) const {
+#pragma unroll
+    for (int n = 0; n < NI; ++n)
+      lds_dma16(__builtin_amdgcn_readfirstlane(lds_base + (NI * w + n) * 1024),
+                base + off[n] + (row[n] >= na ? skip : 0u), view);
+  }
+};
 
 // --------------------------------------------------------------- dq, LSE, D
 // Tile: 128 rows of one (consumer, sequence, query head), 32 per wave; S^T = K q^T and
@@ -134,9 +143,11 @@ __global__ __launch_bounds__(64 * kReachBwdWaves) void reach_bwd_dq_kernel(Reach
   f32x16 dq[NDT];
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt) dq[dt] = zero16();
+  const ReachCopy<DH, BLK, NW> cp(ROW, w, lane);
   auto fetch = [&](int j, uint32_t at) {
-    reach_copy<DH, BLK, NW>(at, kv, ROW, j * BLK, na, skip, n, w, lane);
-    reach_copy<DH, BLK, NW>(at + BLK * ROW, vv, ROW, j * BLK, na, skip, n, w, lane);
+    const int left = na - j * BLK;  // first slots from the block's start on
+    cp.go(at, kv, (uint32_t)j * BLK * ROW, w, left, (uint32_t)skip * ROW);
+    cp.go(at + BLK * ROW, vv, (uint32_t)j * BLK * ROW, w, left, (uint32_t)skip * ROW);
   };
   if (nblk > 0) fetch(0, lbase);
   for (int j = 0; j < nblk; ++j) {
@@ -227,16 +238,22 @@ __global__ __launch_bounds__(64 * kReachBwdWaves) void reach_bwd_dq_kernel(Reach
 
 // The products of 32 rows (block at kb: queries, then dO at kb + dofs) with the 32 slots whose K and
 // V rows are kf, vf: P and dS of the rows that `sees` says read the slot (lane (h, r): slot r, rows
-// 8 (i / 4) + 4 h + i % 4), then dv^T += dO^T P, dk^T += Q^T dS. lz, dz: the rows' LSE and D.
+// 8 (i / 4) + 4 h + i % 4), then dv^T += dO^T P, dk^T += Q^T dS. lz, nz: the rows' LSE and -D.
 template <int DH, class F>
 __device__ __forceinline__ void reach_bwd_rows(const char* sm, const PfLane<DH>& lo, uint32_t kb,
                                                uint32_t dofs, const bf16x8 (&kf)[DH / 16],
                                                const bf16x8 (&vf)[DH / 16], const float* lz,
-                                               const float* dz, float cl2, int h, bool masked,
+                                               const float* nz, float cl2, int h, bool masked,
                                                F sees, f32x16 (&dk)[DH / 32],
                                                f32x16 (&dv)[DH / 32]) {
   constexpr int NKS = DH / 16, NDT = DH / 32;
-  f32x16 sc = zero16(), dp = zero16();
+  f32x16 sc = zero16(), dp;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const f32x4 d4 = *(const f32x4*)(nz + 8 * g + 4 * h);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dp[4 * g + e] = d4[e];
+  }
 #pragma unroll
   for (int ks = 0; ks < NKS; ++ks) {
     sc = mma32(sc, pf_ldk<DH>(sm, lo, kb, ks), kf[ks]);
@@ -266,12 +283,7 @@ __device__ __forceinline__ void reach_bwd_rows(const char* sm, const PfLane<DH>&
 #pragma unroll
       for (int u = 0; u < 3; ++u) dv[dt] = mma32(dv[dt], f, pw[u][kh]);
     }
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    const f32x4 d4 = *(const f32x4*)(dz + 8 * g + 4 * h);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) dp[4 * g + e] = sc[4 * g + e] * (dp[4 * g + e] - d4[e]);
-  }
+  dp *= sc;
   cut24(dp, pw);
 #pragma unroll
   for (int kh = 0; kh < 2; ++kh)
@@ -284,10 +296,13 @@ __device__ __forceinline__ void reach_bwd_rows(const char* sm, const PfLane<DH>&
 }
 
 // ------------------------------------------------------------------- dk, dv
-// Tile: 128 slots of one (channel, sequence, KV head), 32 per wave, whose K and V rows stay in
-// registers as the column operand. It walks every block of 64 rows whose windows hold some of its
+// Tile: 64 slots of one (channel, sequence, KV head), 32 per pair of waves, whose K and V rows stay
+// in registers as the column operand. It walks every block of 64 rows whose windows hold some of its
 // slots, for every consumer of the channel and every query head of the KV head, the next block
-// copied into LDS while the current one is multiplied.
+// copied into LDS while the current one is multiplied; a pair's waves take a half of each block, and
+// their sums meet in LDS at the end. (One wave per 32 slots, 128 per tile, walks window + 128 rows for
+// the window + 32 that each wave needs, and leaves the last of two rounds of workgroups half
+// empty: 2 x 2048 tokens, 16 layers of 6/3 heads of 96, window 512 414 us, this way 322.)
 template <int DH>
 __global__ __launch_bounds__(64 * kReachBwdWaves) __attribute__((amdgpu_waves_per_eu(2)))
 void reach_bwd_dkv_kernel(ReachBwdArgs a) {
@@ -308,9 +323,11 @@ void reach_bwd_dkv_kernel(ReachBwdArgs a) {
   const int pos0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq;
   const int pq = pos0 + (a.mask_paper ? 0 : 1);  // row i reads slots below pq + gs i
   const int send = pos0 + a.gs * (a.T - 1) + 1;  // slots written: [0, send)
-  const int sbase = stile * 32 * NW;
+  constexpr int SLOTS = 32 * NW / 2;
+  const int sbase = stile * SLOTS;
   if (sbase >= send) return;
-  const int ws0 = sbase + 32 * w, slot = ws0 + r;
+  const int pair = w & 1, half = w >> 1;  // this wave's slots, its half of every block
+  const int ws0 = sbase + 32 * pair, slot = ws0 + r;
   const bool slot_ok = slot < send;
 
   const long cbase = (((long)c * a.B + b) * a.Hkv + kvh) * (long)a.S_cap * DH;
@@ -329,14 +346,15 @@ void reach_bwd_dkv_kernel(ReachBwdArgs a) {
 #pragma unroll
   for (int dt = 0; dt < NDT; ++dt) dk[dt] = dv[dt] = zero16();
   const PfLane<DH> lo = pf_lane<DH>(lane);
-  // rows i with sbase < pq + gs i (the first) and pq + gs i - window <= sbase + 32 NW - 1
-  const int i_num = sbase - pq, l_num = sbase + 32 * NW - 1 + a.window - pq;
+  // rows i with sbase < pq + gs i (the first) and pq + gs i - window <= sbase + SLOTS - 1
+  const int i_num = sbase - pq, l_num = sbase + SLOTS - 1 + a.window - pq;
   const int i_first = i_num < 0 ? 0 : i_num / a.gs + 1;
   const int i_last = l_num < 0 ? -1 : min(l_num / a.gs, a.T - 1);
   const int qb0 = i_first / QB, nqb = i_last >= i_first ? i_last / QB - qb0 + 1 : 0;
   const int nit = (a.grp.offsets[c + 1] - a.grp.offsets[c]) * G * nqb;
   const uint32_t ostride = (uint32_t)a.Hq * DH * 2u;
-  float lse_n = 0.f, dlt_n = 0.f;  // the next block's row statistics (threads < QB)
+  const ReachCopy<DH, QB, NW> cq(ROW, w, lane), cd(ostride, w, lane);
+  float lse_n = 0.f, dlt_n = 0.f;  // the next block's LSE and -D of row tid (threads < QB)
   auto fetch = [&](int it, uint32_t buf) {
     const int qb = qb0 + it % nqb, x = it / nqb, hq = kvh * G + x % G;
     const int l = a.grp.members[a.grp.offsets[c] + x / G];
@@ -344,12 +362,12 @@ void reach_bwd_dkv_kernel(ReachBwdArgs a) {
     const long rowl = ((long)l * a.B + b) * a.T;
     const auto qv = make_view(a.Q + rows0 * DH, (uint32_t)a.T * DH * 2u);
     const auto dov = make_view(a.dO + rowl * a.Hq * DH + (long)hq * DH, (uint32_t)a.T * ostride);
-    reach_copy<DH, QB, NW>(buf, qv, DH * 2u, qb * QB, a.T, 0, a.T, w, lane);
-    reach_copy<DH, QB, NW>(buf + QB * ROW, dov, ostride, qb * QB, a.T, 0, a.T, w, lane);
+    cq.go(buf, qv, (uint32_t)(qb * QB) * ROW, w);
+    cd.go(buf + QB * ROW, dov, (uint32_t)(qb * QB) * ostride, w);
     if (tid < QB) {
       const int qr = qb * QB + tid;
       lse_n = qr < a.T ? a.lse[rows0 + qr] : 1.0e30f;  // a row past T weighs 0
-      dlt_n = qr < a.T ? a.dlt[rows0 + qr] : 0.f;
+      dlt_n = qr < a.T ? -a.dlt[rows0 + qr] : 0.f;
     }
   };
   if (nit > 0) fetch(0, lbase);
@@ -364,22 +382,45 @@ void reach_bwd_dkv_kernel(ReachBwdArgs a) {
     __syncthreads();  // block it is in LDS; every wave is done with block it - 1
     const int qb = qb0 + it % nqb;
     if (it + 1 < nit) fetch(it + 1, lbase + (kb ^ BUF));
-#pragma unroll
-    for (int hg = 0; hg < 2; ++hg) {
-      const int qg = qb * QB + 32 * hg, qe = min(qg + 31, a.T - 1);  // the half's rows
-      const int lim0 = pq + a.gs * qg, lim1 = pq + a.gs * qe;
-      if (qg < a.T && lim1 > ws0 && lim0 - a.window <= ws0 + 31) {
-        const bool masked = lim0 <= ws0 + 31 || lim1 - a.window > ws0;
-        reach_bwd_rows<DH>(smem, lo, kb + hg * 32 * ROW, QB * ROW, kf, vf, &s_lse[u][32 * hg],
-                           &s_dlt[u][32 * hg], a.scale_log2, h, masked,
-                           [&](int x) {
-                             const int lim = lim0 + a.gs * x;
-                             return slot < lim && slot >= lim - a.window;
-                           },
-                           dk, dv);
-      }
+    const int qg = qb * QB + 32 * half, qe = min(qg + 31, a.T - 1);  // this wave's rows
+    const int lim0 = pq + a.gs * qg, lim1 = pq + a.gs * qe;
+    if (qg < a.T && lim1 > ws0 && lim0 - a.window <= ws0 + 31) {
+      const bool masked = lim0 <= ws0 + 31 || lim1 - a.window > ws0;
+      reach_bwd_rows<DH>(smem, lo, kb + half * 32 * ROW, QB * ROW, kf, vf, &s_lse[u][32 * half],
+                         &s_dlt[u][32 * half], a.scale_log2, h, masked,
+                         [&](int x) {
+                           const int lim = lim0 + a.gs * x;
+                           return slot < lim && slot >= lim - a.window;
+                         },
+                         dk, dv);
     }
   }
+  // the second halves' sums through LDS: dk^T and dv^T of 32 slots per pair, as the registers lie
+  __syncthreads();
+  static_assert(2 * 2 * 64 * 16 * NDT * 4 <= 2 * BUF, "both pairs' sums fit the blocks");
+  f32x4* so = (f32x4*)smem + pair * 2 * NDT * 4 * 64 + lane;
+  if (half == 1) {
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x4 kq, vq;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kq[i] = dk[dt][4 * g + i], vq[i] = dv[dt][4 * g + i];
+        so[(2 * (4 * dt + g)) * 64] = kq;
+        so[(2 * (4 * dt + g) + 1) * 64] = vq;
+      }
+  }
+  __syncthreads();
+  if (half == 1) return;
+#pragma unroll
+  for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 kq = so[(2 * (4 * dt + g)) * 64], vq = so[(2 * (4 * dt + g) + 1) * 64];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dk[dt][4 * g + i] += kq[i], dv[dt][4 * g + i] += vq[i];
+    }
   if (slot_ok) {
     float* dkd = a.dKc + cbase + (long)slot * DH;
     float* dvd = a.dVc + cbase + (long)slot * DH;
@@ -453,7 +494,7 @@ void reach_bwd_sink_kernel(ReachBwdArgs a) {
   const uint32_t ostride = (uint32_t)a.Hq * DH * 2u;
   char* ring = smem + w * RING;
   const uint32_t ring_at = (uint32_t)(uintptr_t)ring;
-  float lse_n = 0.f, dlt_n = 0.f;  // the next step's row r
+  float lse_n = 0.f, dlt_n = 0.f;  // LSE and -D of the next step's row r
   auto fetch = [&](int j, int st) {  // step j of this wave into ring stage st
     const int it = gw + stride * j, qb = qb0 + it % nqb, x = it / nqb, hq = kvh * G + x % G;
     const int l = a.grp.members[a.grp.offsets[c] + x / G];
@@ -472,7 +513,7 @@ void reach_bwd_sink_kernel(ReachBwdArgs a) {
     }
     const int qr = qb * 32 + r;
     lse_n = qr < a.T ? a.lse[rows0 + qr] : 1.0e30f;  // a row past T weighs 0
-    dlt_n = qr < a.T ? a.dlt[rows0 + qr] : 0.f;
+    dlt_n = qr < a.T ? -a.dlt[rows0 + qr] : 0.f;
   };
   if (mine > 0) fetch(0, 0);
   for (int j = 0; j < mine; ++j) {
@@ -549,9 +590,9 @@ size_t reach_backward_bytes(const Shape& sh) {
 
 template <int DH>
 static void reach_backward(ReachBwdArgs a, const Shape& sh, hipStream_t s) {
-  const int rows = 32 * kReachBwdWaves, slices = sh.k * sh.B * sh.Hkv;
+  const int rows = 32 * kReachBwdWaves, slots = rows / 2, slices = sh.k * sh.B * sh.Hkv;
   a.n_qtiles = (sh.T_new + rows - 1) / rows;
-  a.n_stiles = (int)(((long)sh.ctx_max + sh.span() + rows - 1) / rows);
+  a.n_stiles = (int)(((long)sh.ctx_max + sh.span() + slots - 1) / slots);
   const dim3 blk(64 * kReachBwdWaves);
   hipLaunchKernelGGL(reach_bwd_dq_kernel<DH>,
                      dim3((unsigned)(a.n_qtiles * sh.Hq * sh.B * sh.L)), blk, 0, s, a);
@@ -561,8 +602,9 @@ static void reach_backward(ReachBwdArgs a, const Shape& sh, hipStream_t s) {
   const long first = std::min<long>(a.sinks, past);
   if (first <= 0) return;
   a.n32 = (int)((first + 31) / 32);
-  // chunks of rows until the workgroups fill the CUs twice, as far as the partial sums' room goes
-  const long per = (long)slices * a.n32, want = (2L * device_cus() + per - 1) / per;
+  // chunks of rows while the workgroups fit the CUs at once (LDS: two of them at head dim 64, one at
+  // 96), as far as the partial sums' room goes
+  const long per = (long)slices * a.n32, want = (DH == 64 ? 2L : 1L) * device_cus() / per;
   const long steps = ((long)sh.L / sh.k + 1) * (sh.Hq / sh.Hkv) * ((sh.T_new + 31) / 32);
   a.chunks = (int)std::max(1L, std::min({want, (long)(kSinkParts / a.n32), steps / 4}));
   if (a.chunks == 1) a.part = nullptr;
