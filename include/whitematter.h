@@ -499,14 +499,20 @@ int wm_channel_attend_window_backward(const wm_dims *dims, const wm_params *para
  *   seq         0 <= seq < B
  *   prefix_len  1 <= prefix_len <= min(S_cap, P_cap)
  *   Kp, Vp      device [k][Hkv][P_cap][d] in dtype, apart from Kc and Vc; slots at and past
- *               prefix_len are left as they are */
+ *               prefix_len are left as they are
+ *   Kd, Kd_out  device [k][Hkv][d] in dtype, or both NULL: the dummy keys, and the same turned
+ *               back. A dummy key is stored without RoPE, so its score depends on where the
+ *               query's own positions start: for the scores of the whole sequence, params->Kd of
+ *               wm_channel_attend_shared in WM_MASK_PAPER is Kd_out. */
 int wm_prefix_share(const wm_dims *dims, const void *Kc, const void *Vc, int32_t seq,
-                    int32_t prefix_len, int32_t P_cap, void *Kp, void *Vp, wm_stream_t stream);
+                    int32_t prefix_len, int32_t P_cap, void *Kp, void *Vp, const void *Kd,
+                    void *Kd_out, wm_stream_t stream);
 
 /* wm_channel_attend for a batch whose sequences share a prefix: every row reads the
  * prefix_len slots of its channel and KV head in Kp, Vp and, of its own sequence's cache, the
  * slots wm_channel_attend lets it read; one softmax over both and the dummy slot. ctx_len and
- * the positions count the sequence's own tokens, from 0 after the prefix.
+ * the positions count the sequence's own tokens, from 0 after the prefix; the dummy key is used
+ * as given (wm_prefix_share turns it to match).
  *   prefix_len  0 <= prefix_len <= P_cap (0: Kp and Vp are not read and may be NULL)
  *   Kp, Vp      device [k][Hkv][P_cap][d] in dtype (see wm_prefix_share)
  * Few new tokens (T_new <= 4): the prefix is read once for the whole batch. Other arguments
@@ -539,7 +545,8 @@ int wm_channel_attend_weigh(const wm_dims *dims, const wm_params *params, const 
  * the lower slot; NaN counts as the smallest), in slot order; shorter sequences keep all. The
  * j-th kept slot, from slot s, becomes slot j: its key turned by j - s positions (so that slot =
  * position holds again and every other call continues from ctx_out), rounded to dtype once;
- * its value and weight as they are.
+ * its value and weight as they are. Later queries count positions from ctx_out: their distances to
+ * the kept slots are the new ones, and so is the position at which they meet the dummy.
  *   dims        B, k, Hkv, d, S_cap, ctx_max, dtype, rope_theta (T_new is not used)
  *   ctx_len     device int32 [B] in [0, ctx_max] or NULL (empty sequences)
  *   keep        >= 1, first >= 0, recent >= 0, first + recent <= keep

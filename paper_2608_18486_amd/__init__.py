@@ -103,7 +103,7 @@ def lib() -> ctypes.CDLL:
                                      _vp],
         "wm_channel_attend_window_backward": [D, P, _vp, _i32p, _vp, _i32, _i32, _vp, _vp, _vp,
                                               _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
-        "wm_prefix_share": [D, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp],
+        "wm_prefix_share": [D, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp],
         "wm_channel_attend_shared": [D, P, _vp, _i32p, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
                                      _vp, _sz, _vp],
         "wm_channel_attend_weigh": [D, P, _vp, _i32p, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp],
@@ -417,7 +417,9 @@ def _want(name, t, shape, dtype):
     if t.shape != shape or t.dtype != dtype:
         raise ValueError("%s must be %s of shape %s, got %s of shape %s" %
                          (name, dtype, shape, t.dtype, tuple(t.shape)))
-    return _ptr(t)
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
 
 
 def _elem(dims):
@@ -464,15 +466,19 @@ def channel_attend_window_backward(dims: Dims, params, Q, chan_map, ctx_len, win
                                                    *out, wp, wn, _stream(stream)))
 
 
-def prefix_share(dims: Dims, Kc, Vc, seq: int, prefix_len: int, Kp, Vp, stream=None):
+def prefix_share(dims: Dims, Kc, Vc, seq: int, prefix_len: int, Kp, Vp, Kd=None, Kd_out=None,
+                 stream=None):
     """Slots [0, prefix_len) of sequence seq into Kp, Vp [k, Hkv, P_cap, d], the keys turned
-    back by prefix_len positions: the prefix that channel_attend_shared reads."""
+    back by prefix_len positions: the prefix that channel_attend_shared reads. Kd_out
+    (optional): the dummy keys Kd turned back likewise, for its params."""
     kc, vc = _cache_ptrs(dims, Kc=Kc, Vc=Vc)
     P_cap = Kp.shape[2] if Kp is not None and Kp.dim() == 4 else 0
     kp, vp = (_want(n, t, (dims.k, dims.Hkv, P_cap, dims.d), _elem(dims))
               for n, t in (("Kp", Kp), ("Vp", Vp)))
-    _check(lib().wm_prefix_share(ctypes.byref(dims), kc, vc, seq, prefix_len, P_cap, kp, vp,
-                                 _stream(stream)))
+    kd, ko = (_want(n, t, (dims.k, dims.Hkv, dims.d), _elem(dims))
+              for n, t in (("Kd", Kd), ("Kd_out", Kd_out)))
+    _check(lib().wm_prefix_share(ctypes.byref(dims), kc, vc, seq, prefix_len, P_cap, kp, vp, kd,
+                                 ko, _stream(stream)))
 
 
 def shared_workspace(dims: Dims, prefix_len: int) -> int:

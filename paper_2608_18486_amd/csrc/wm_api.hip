@@ -1868,7 +1868,8 @@ int wm_channel_attend_window_backward(const wm_dims* dims, const wm_params* para
 }
 
 int wm_prefix_share(const wm_dims* dims, const void* Kc, const void* Vc, int32_t seq,
-                    int32_t prefix_len, int32_t P_cap, void* Kp, void* Vp, wm_stream_t stream) {
+                    int32_t prefix_len, int32_t P_cap, void* Kp, void* Vp, const void* Kd,
+                    void* Kd_out, wm_stream_t stream) {
   WM_TRY(validate_dims(dims, WM_OP_PREFIX_SHARE, nullptr));
   const wm_dims& d = *dims;
   if (seq < 0 || seq >= d.B) return fail(WM_ERR_ARG, "seq must be in [0, B)");
@@ -1887,8 +1888,16 @@ int wm_prefix_share(const wm_dims* dims, const void* Kc, const void* Vc, int32_t
   if (overlap(Kp, to, Vp, to) || overlap(Kp, to, Kc, from) || overlap(Kp, to, Vc, from) ||
       overlap(Vp, to, Kc, from) || overlap(Vp, to, Vc, from))
     return fail(WM_ERR_ARG, "Kp and Vp must not overlap the cache or each other");
+  if (Kd || Kd_out) {
+    WM_TRY(need_ptr(Kd, "Kd"));
+    WM_TRY(need_ptr(Kd_out, "Kd_out"));
+    if (overlap(Kd, row, Kd_out, row) || overlap(Kd_out, row, Kp, to) ||
+        overlap(Kd_out, row, Vp, to) || overlap(Kd_out, row, Kc, from) ||
+        overlap(Kd_out, row, Vc, from) || overlap(Kd, row, Kp, to) || overlap(Kd, row, Vp, to))
+      return fail(WM_ERR_ARG, "Kd_out must not overlap the other tensors, nor Kp and Vp Kd");
+  }
   (void)hipGetLastError();
-  wm::launch_prefix_share(make_shape(d), Kc, Vc, seq, prefix_len, P_cap, Kp, Vp,
+  wm::launch_prefix_share(make_shape(d), Kc, Vc, seq, prefix_len, P_cap, Kp, Vp, Kd, Kd_out,
                           d.dtype == WM_BF16, (hipStream_t)stream);
   return launched();
 }

@@ -227,8 +227,8 @@ __device__ __forceinline__ void decode_block(const DecodeArgs<bf16>& a, const in
     for (int n = 0; n < 2 * C::NI; ++n) {
       uint32_t o = base + coff[n % C::NI];
       if constexpr (WIN)
-        o += at + (64 * (n % C::NI) + lane) / C::CPR >= ws.na ? (uint32_t)ws.skip * C::ROW_BYTES
-                                                              : 0u;
+        o += j < nw && at + (64 * (n % C::NI) + lane) / C::CPR >= ws.na
+                 ? (uint32_t)ws.skip * C::ROW_BYTES : 0u;
       const uint32_t lds =
           __builtin_amdgcn_readfirstlane(ring_at + st * C::STAGE + 1024 * n);
       if constexpr (ONCE) lds_dma16_stream(lds, o, n < C::NI ? kview : vview);

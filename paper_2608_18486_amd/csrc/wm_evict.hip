@@ -212,15 +212,52 @@ struct MoveArgs {
   double log2_theta;
 };
 
+// Two halves of 8 elements of a key, from element e of each half on, turned by `by` positions.
+__device__ __forceinline__ void turn8(float (&x1)[8], float (&x2)[8], double by,
+                                      const double* turn) {
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    const double t = by * turn[u];
+    float sn, cs;
+    sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
+    const float p = x1[u], q = x2[u];
+    x1[u] = p * cs - q * sn;
+    x2[u] = q * cs + p * sn;
+  }
+}
+// Turns per position of a key's element pairs.
+template <int DH> __device__ __forceinline__ void turn_table(double* turn, double log2_theta) {
+  for (int m = threadIdx.x; m < DH / 2; m += 256)
+    turn[m] = exp2(log2_theta * (-2.0 * (double)m / (double)DH)) * 0.15915494309189533577;
+  __syncthreads();
+}
+
+// y = the rows x turned by `by` positions.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void turn_rows_kernel(const T* x, T* y, long rows, int by,
+                                                        double log2_theta) {
+  constexpr int H = DH / 2, C = H / 8;
+  __shared__ double turn[H];
+  turn_table<DH>(turn, log2_theta);
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * C) return;
+  const long row = i / C;
+  const int e = (int)(i % C) * 8;
+  float x1[8], x2[8];
+  load8(x + row * DH + e, x1);
+  load8(x + row * DH + H + e, x2);
+  turn8(x1, x2, (double)by, turn + e);
+  store8(y + row * DH + e, x1);
+  store8(y + row * DH + H + e, x2);
+}
+
 // Rows [0, n) of every destination slice: a thread moves 8 elements of the key's first half,
 // the 8 they rotate with, and the same of the value.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void move_rows_kernel(MoveArgs a) {
   constexpr int H = DH / 2, C = H / 8;  // threads per row
-  __shared__ double turn[H];            // turns per position
-  for (int m = threadIdx.x; m < H; m += 256)
-    turn[m] = exp2(a.log2_theta * (-2.0 * (double)m / (double)DH)) * 0.15915494309189533577;
-  __syncthreads();
+  __shared__ double turn[H];
+  turn_table<DH>(turn, a.log2_theta);
   const int slice = blockIdx.y;  // destination (channel, sequence, KV head)
   const int h = slice % a.Hkv, b = slice / a.Hkv % a.nb, c = slice / (a.Hkv * a.nb);
   const int n = a.idx ? min(ctx_at(a.ctx_len, a.b0 + b, a.ctx_max), a.keep) : a.keep;
@@ -238,16 +275,7 @@ __global__ __launch_bounds__(256) void move_rows_kernel(MoveArgs a) {
     load8(K + (long)s * DH + H + e, x2);
     const frag_t<T> v1 = ld_frag<T>(V + (long)s * DH + e);
     const frag_t<T> v2 = ld_frag<T>(V + (long)s * DH + H + e);
-    const double by = (double)(j + a.shift - s);
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const double t = by * turn[e + u];
-      float sn, cs;
-      sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
-      const float p = x1[u], q = x2[u];
-      x1[u] = p * cs - q * sn;
-      x2[u] = q * cs + p * sn;
-    }
+    turn8(x1, x2, (double)(j + a.shift - s), turn + e);
     store8(Ko + (long)j * DH + e, x1);
     store8(Ko + (long)j * DH + H + e, x2);
     st_frag<T>(Vo + (long)j * DH + e, v1);
@@ -290,12 +318,29 @@ void launch_evict(const Shape& sh, const int32_t* ctx_len, int keep, int first, 
   else move_rows<float>(m, sh.k, sh.d, s);
 }
 
+template <typename T>
+static void turn_rows(const Shape& sh, const T* x, T* y, int by, hipStream_t s) {
+  const long rows = (long)sh.k * sh.Hkv;
+  const double lt = log2((double)sh.rope_theta);
+  const dim3 grid((unsigned)((rows * (sh.d / 16) + 255) / 256));
+  if (sh.d == 32)
+    hipLaunchKernelGGL((turn_rows_kernel<T, 32>), grid, dim3(256), 0, s, x, y, rows, by, lt);
+  else if (sh.d == 64)
+    hipLaunchKernelGGL((turn_rows_kernel<T, 64>), grid, dim3(256), 0, s, x, y, rows, by, lt);
+  else
+    hipLaunchKernelGGL((turn_rows_kernel<T, 96>), grid, dim3(256), 0, s, x, y, rows, by, lt);
+}
+
 void launch_prefix_share(const Shape& sh, const void* Kc, const void* Vc, int seq, int len,
-                         int P_cap, void* Kp, void* Vp, bool bf, hipStream_t s) {
+                         int P_cap, void* Kp, void* Vp, const void* Kd, void* Kd_out, bool bf,
+                         hipStream_t s) {
   const MoveArgs m{Kc, Vc, Kp, Vp, nullptr, nullptr, sh.B, sh.Hkv, sh.S_cap, P_cap, 0, len, 0,
                    seq, 1, -len, log2((double)sh.rope_theta)};
   if (bf) move_rows<bf16>(m, sh.k, sh.d, s);
   else move_rows<float>(m, sh.k, sh.d, s);
+  if (!Kd_out) return;
+  if (bf) turn_rows<bf16>(sh, (const bf16*)Kd, (bf16*)Kd_out, -len, s);
+  else turn_rows<float>(sh, (const float*)Kd, (float*)Kd_out, -len, s);
 }
 
 }  // namespace wm

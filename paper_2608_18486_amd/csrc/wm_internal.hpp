@@ -339,7 +339,8 @@ void launch_evict(const Shape& sh, const int32_t* ctx_len, int keep, int first, 
                   int32_t* ctx_out, float* weight_out, void* Ko, void* Vo, int32_t* kept,
                   int32_t* idx, bool bf, hipStream_t s);
 void launch_prefix_share(const Shape& sh, const void* Kc, const void* Vc, int seq, int len,
-                         int P_cap, void* Kp, void* Vp, bool bf, hipStream_t s);
+                         int P_cap, void* Kp, void* Vp, const void* Kd, void* Kd_out, bool bf,
+                         hipStream_t s);
 
 // -- measurement helper ---------------------------------------------------------
 // blocks x 4 waves, each issuing 8 * iters independent 32x32x16 bf16 MFMAs on small

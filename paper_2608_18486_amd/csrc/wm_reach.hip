@@ -442,7 +442,7 @@ void reach_few_kernel(ReachArgs<bf16> a) {
     for (int n = 0; n < 2 * NI; ++n) {
       uint32_t o = base + coff[n % NI];
       if constexpr (!PRE)
-        o += at + (64 * (n % NI) + lane) / CPR >= sp.na ? (uint32_t)sp.skip * ROW : 0u;
+        o += j < nw && at + (64 * (n % NI) + lane) / CPR >= sp.na ? (uint32_t)sp.skip * ROW : 0u;
       const uint32_t to = __builtin_amdgcn_readfirstlane(ring_at + st * STAGE + 1024 * n);
       if constexpr (PRE) lds_dma16(to, o, pre ? (n < NI ? kpview : vpview) : (n < NI ? kview : vview));
       else lds_dma16(to, o, n < NI ? kview : vview);

@@ -101,10 +101,11 @@ def test_weigh_refusals(wm):
     assert _call(wm, "wm_channel_attend_weigh", _dims(wm), after=(None,)) == wm.ERR_ARG
 
 
-def _share(wm, dims, seq=0, n=4, cap=16, ptrs=(0, 1, 2, 3)):
+def _share(wm, dims, seq=0, n=4, cap=16, ptrs=(0, 1, 2, 3), kd=(None, None)):
     return wm.lib().wm_prefix_share(ctypes.byref(dims), *[None if p is None else _at(p)
                                                           for p in ptrs[:2]], seq, n, cap,
-                                    *[None if p is None else _at(p) for p in ptrs[2:]], None)
+                                    *[None if p is None else _at(p) for p in (*ptrs[2:], *kd)],
+                                    None)
 
 
 def test_prefix_share_refusals(wm):
@@ -112,7 +113,10 @@ def test_prefix_share_refusals(wm):
     for kw, code in ((dict(seq=-1), "ERR_ARG"), (dict(seq=2), "ERR_ARG"), (dict(n=0), "ERR_ARG"),
                      (dict(n=33, cap=64), "ERR_CAPACITY"), (dict(n=17), "ERR_CAPACITY"),
                      (dict(cap=1 << 25), "ERR_SHAPE"), (dict(ptrs=(0, 1, 0, 3)), "ERR_ARG"),
-                     (dict(ptrs=(0, 1, 2, 2)), "ERR_ARG"), (dict(ptrs=(0, 1, 2, 1)), "ERR_ARG")):
+                     (dict(ptrs=(0, 1, 2, 2)), "ERR_ARG"), (dict(ptrs=(0, 1, 2, 1)), "ERR_ARG"),
+                     (dict(kd=(4, None)), "ERR_ARG"), (dict(kd=(None, 4)), "ERR_ARG"),
+                     (dict(kd=(4, 4)), "ERR_ARG"), (dict(kd=(4, 1)), "ERR_ARG"),
+                     (dict(kd=(2, 5)), "ERR_ARG")):
         assert _share(wm, d, **kw) == getattr(wm, code), kw
     for i in range(4):
         assert _share(wm, d, ptrs=[None if i == j else j for j in range(4)]) == wm.ERR_ARG

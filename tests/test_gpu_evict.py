@@ -123,8 +123,12 @@ def test_prefix_share(wm, dtype, d, P, P_cap, seq):
                         dtype=wm.BF16 if dtype == "bf16" else wm.F32)
     Kp = torch.full((k, Hkv, P_cap, d), float("nan"), dtype=Kc.dtype, device="cuda")
     Vp = torch.full_like(Kp, float("nan"))
-    wm.prefix_share(dims, Kc.cuda(), Vc.cuda(), seq, P, Kp, Vp)
+    Kd = torch.randn((k, Hkv, d), generator=torch.Generator().manual_seed(4)).to(Kc.dtype)
+    Kd_out = torch.full_like(Kd, float("nan"), device="cuda")
+    wm.prefix_share(dims, Kc.cuda(), Vc.cuda(), seq, P, Kp, Vp, Kd=Kd.cuda(), Kd_out=Kd_out)
     torch.cuda.synchronize()
+    _check_keys(Kd_out.cpu().double().numpy().reshape(-1, d), Kd.double().numpy().reshape(-1, d),
+                np.full(k * Hkv, -P), dtype, "dummy")
     for c in range(k):
         for h in range(Hkv):
             _check_keys(Kp[c, h, :P].cpu().double().numpy(), Kc[c, seq, h, :P].double().numpy(),
