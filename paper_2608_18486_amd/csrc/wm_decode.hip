@@ -70,7 +70,6 @@ template <typename T> struct DecodeArgs {
   LayerTable live;
   ChannelGroups cg;
   int window, sinks;  // WIN kernels: a row reads its last `window` slots and the first `sinks`
-  int split0;         // this kernel's first split among a row's nsplit partial states
   // weighed attention: raw scores of every row and slot [L][B][Hq][T_new][s_ld] (hidden: -1e30),
   // and the rows' log-sum-exp in log2 units; else null
   float *scores, *lse;
@@ -221,13 +220,13 @@ __device__ __forceinline__ void decode_block(const DecodeArgs<bf16>& a, const in
   // block j of this wave into ring stage st (blocks past the wave's last are copied as
   // zeros, so the count of copies in flight is the same at every wait)
   auto issue = [&](int j, int st) {
-    const int at = s0 + C::BKV * (w + C::NW * j);
-    const uint32_t base = j < nw ? (uint32_t)at * C::ROW_BYTES : kOffOob;
+    const uint32_t base =
+        j < nw ? (uint32_t)(s0 + C::BKV * (w + C::NW * j)) * C::ROW_BYTES : kOffOob;
 #pragma unroll
     for (int n = 0; n < 2 * C::NI; ++n) {
       uint32_t o = base + coff[n % C::NI];
       if constexpr (WIN)
-        o += j < nw && at + (64 * (n % C::NI) + lane) / C::CPR >= ws.na
+        o += j < nw && s0 + C::BKV * (w + C::NW * j) + (64 * (n % C::NI) + lane) / C::CPR >= ws.na
                  ? (uint32_t)ws.skip * C::ROW_BYTES : 0u;
       const uint32_t lds =
           __builtin_amdgcn_readfirstlane(ring_at + st * C::STAGE + 1024 * n);
@@ -349,7 +348,7 @@ __device__ __forceinline__ void decode_block(const DecodeArgs<bf16>& a, const in
       ow += sw[gi * C::OLD + dd] * al;
     }
     int i;
-    float* dst = a.part + (row_of(g0 + gi, i) * a.nsplit + a.split0 + split) * (DH + 2);
+    float* dst = a.part + (row_of(g0 + gi, i) * a.nsplit + split) * (DH + 2);
     dst[dd] = ow;
     if (dd == 0) {
       dst[DH] = M;
@@ -532,7 +531,7 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
       int i = g % a.T_new, gq = (g / a.T_new) % grp, mi = g / (a.T_new * grp);
       int l = a.cg.members[off + mi], hq = kvh * grp + gq;
       long rid = (((long)l * a.B + b) * a.Hq + hq) * a.T_new + i;
-      float* dst = a.part + (rid * a.nsplit + a.split0 + split) * (DH + 2);
+      float* dst = a.part + (rid * a.nsplit + split) * (DH + 2);
       dst[dd] = Osum;
       if (dd == 0) {
         dst[DH] = M;
@@ -544,7 +543,7 @@ __global__ __launch_bounds__(256) void attend_decode_kernel(DecodeArgs<T> a) {
 }
 
 // One wave per query row: fold the dummy slot and all split partials.
-template <typename T, int DH>
+template <typename T, int DH, bool LSE = false>
 __global__ __launch_bounds__(256) void attend_combine_kernel(DecodeArgs<T> a) {
   constexpr int EPL = (DH + 63) / 64;  // elements per lane: channel 64 e + lane
   const long rows = (long)a.L * a.B * a.Hq * a.T_new;
@@ -587,7 +586,7 @@ __global__ __launch_bounds__(256) void attend_combine_kernel(DecodeArgs<T> a) {
   T* dst = a.O + ((((long)l * a.B + b) * a.T_new + i) * a.Hq + hq) * DH;
   for (int e = 0; e < EPL; ++e)
     if (active(e)) dst[64 * e + lane] = from_f32<T>(o[e] / Lsum);
-  if (a.lse && lane == 0) a.lse[rid] = fmaf(M, cl2, __log2f(Lsum));
+  if (LSE && lane == 0) a.lse[rid] = fmaf(M, cl2, __log2f(Lsum));
 }
 
 // weight[c][b][h][s] += the sum over the rows that read (c, b, h) of 2^(score - lse): a thread takes
@@ -632,12 +631,13 @@ __global__ __launch_bounds__(256) void decode_weigh_kernel(DecodeArgs<T> a, floa
 // The workgroups of a prefix's splits and those of the sequences' own caches (decode_block) form
 // one grid: the former are bound by their products and exponentials, the latter by the stream of the
 // cache, and a CU holds some of each at a time. (64 sequences, 24 layers of 16 heads of 64, 4096 + 300
-// slots: 222 us; in two launches, the prefix by waves with rings of their own, 256.)
+// slots: 200 us; in two launches, the prefix by waves with rings of their own, 256.)
 struct PrefixSpan {
   const bf16 *Kp, *Vp;
   int P, P_cap, nsplit, split_len, z;  // z: workgroups of rows per (slice, split)
   int blocks;                          // workgroups of the prefix, ahead of the caches'
   int own, slices;                     // splits and slices of the sequences' own caches
+  float* part;                         // a row's states, the prefix's first
 };
 template <int DH, int RW, int RT> struct PrefixCfg {
   static constexpr int NW = 2, SW = NW / RW, NS = RW == 2 ? 3 : 2;  // SW: waves that cut the slots
@@ -834,7 +834,7 @@ __device__ __forceinline__ void prefix_block(const DecodeArgs<bf16>& a, const Pr
         merge_state(M, lw, &ow, s_b[32 * C::OLD + 2 * gi], s_b[32 * C::OLD + 2 * gi + 1],
                     s_b + gi * C::OLD + dd, 1, cl2);
       }
-      float* dst = a.part + ((long)to * a.nsplit + split) * (DH + 2);
+      float* dst = px.part + ((long)to * a.nsplit + split) * (DH + 2);
       dst[dd] = ow;
       if (dd == 0) {
         dst[DH] = M;
@@ -893,20 +893,20 @@ constexpr long kDecodeMfmaBlocks = 512;
 constexpr long kDecodeStreamBytes = 128L << 20;
 
 // The matrix-core kernel's grid of the sequences' own slots: splits (a.split_len and a.nsplit are
-// set), row tiles, and whether the slots are read once.
+// set, the latter with `more` states of others), row tiles, and whether the slots are read once.
 struct DecodePlan {
   int own, z;
   bool once;
 };
 template <int DH>
-static DecodePlan decode_plan(DecodeArgs<bf16>& a, int G, int nlive, const Shape& sh) {
+static DecodePlan decode_plan(DecodeArgs<bf16>& a, int G, int nlive, const Shape& sh, int more) {
   const int z = std::max(1, (G + 31) / 32);
   const long slices = (long)nlive * sh.B * sh.Hkv * z, kend = (long)sh.ctx_max + sh.span();
   int len = kSplitMax;
   while (len > a.split_len && slices * ((kend + len - 1) / len) < kDecodeMfmaBlocks) len /= 2;
   a.split_len = len;  // at least decode_split_len, so the partials fit their workspace
   const int own = std::max(1, (int)((kend + len - 1) / len));
-  a.nsplit = a.split0 + own;
+  a.nsplit = more + own;
   // a cache read once by one row tile, and larger (all channels: layer by layer, the other
   // layers' calls read theirs in between) than the caches keep from call to call
   const bool once = z == 1 && 4L * sh.k * sh.B * sh.Hkv * kend * DH >= kDecodeStreamBytes;
@@ -914,8 +914,9 @@ static DecodePlan decode_plan(DecodeArgs<bf16>& a, int G, int nlive, const Shape
 }
 
 template <int DH>
-static void decode_mfma(DecodeArgs<bf16>& a, int G, int nlive, const Shape& sh, hipStream_t s) {
-  const auto [own, z, once] = decode_plan<DH>(a, G, nlive, sh);
+static void decode_mfma(DecodeArgs<bf16>& a, int G, int nlive, const Shape& sh, int more,
+                        hipStream_t s) {
+  const auto [own, z, once] = decode_plan<DH>(a, G, nlive, sh, more);
   const long slices = (long)nlive * sh.B * sh.Hkv * z, kend = (long)sh.ctx_max + sh.span();
   const int len = a.split_len;
   const dim3 grid(own, sh.Hkv * sh.B * nlive, z);
@@ -981,33 +982,34 @@ static DecodeArgs<T> decode_args(const Shape& sh, const LayerTable& chan_map,
   return a;
 }
 
-// The splits' partial states from a.split0 on, and with them the states of a row, a.nsplit.
+// The splits' partial states from a.part on; a row has a.nsplit in all, `more` of them others'.
 template <typename T>
-static void decode_states(DecodeArgs<T>& a, const Shape& sh, int G, int nlive, hipStream_t s) {
+static void decode_states(DecodeArgs<T>& a, const Shape& sh, int G, int nlive, int more,
+                          hipStream_t s) {
   if constexpr (sizeof(T) == 2) {  // fp32 at d = 96 is rejected by validation
-    if (sh.d == 96) return decode_mfma<96>(a, G, nlive, sh, s);
-    if (sh.d == 64) return decode_mfma<64>(a, G, nlive, sh, s);
+    if (sh.d == 96) return decode_mfma<96>(a, G, nlive, sh, more, s);
+    if (sh.d == 64) return decode_mfma<64>(a, G, nlive, sh, more, s);
   }
   const dim3 grid(a.nsplit, sh.Hkv * sh.B * nlive);
-  a.nsplit += a.split0;
+  a.nsplit += more;
   if constexpr (sizeof(T) == 4) {
     if (sh.d == 64) return decode_dispatch<T, 64>(a, G, grid, s);
   }
   decode_dispatch<T, 32>(a, G, grid, s);
 }
 
-template <typename T>
+template <typename T, bool LSE = false>
 static void decode_combine(const DecodeArgs<T>& a, int d, hipStream_t s) {
   const long rows = (long)a.L * a.B * a.Hq * a.T_new;
   const dim3 grid((unsigned)((rows + 3) / 4));
   if constexpr (sizeof(T) == 2) {
     if (d == 96) {
-      hipLaunchKernelGGL((attend_combine_kernel<bf16, 96>), grid, dim3(256), 0, s, a);
+      hipLaunchKernelGGL((attend_combine_kernel<bf16, 96, LSE>), grid, dim3(256), 0, s, a);
       return;
     }
   }
-  if (d == 64) hipLaunchKernelGGL((attend_combine_kernel<T, 64>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((attend_combine_kernel<T, 32>), grid, dim3(256), 0, s, a);
+  if (d == 64) hipLaunchKernelGGL((attend_combine_kernel<T, 64, LSE>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((attend_combine_kernel<T, 32, LSE>), grid, dim3(256), 0, s, a);
 }
 
 template <typename T>
@@ -1022,7 +1024,7 @@ void launch_attend_decode(const Shape& shape, const LayerTable& chan_map, const 
   DecodeArgs<T> a = decode_args<T>(sh, chan_map, cg, Q, Kc, Vc, Kd, Vd, ctx_len, doc, partials, O,
                                    &nlive, &G);
   if (reach) a.window = reach->window, a.sinks = reach->sinks;
-  decode_states<T>(a, sh, G, nlive, s);
+  decode_states<T>(a, sh, G, nlive, 0, s);
   decode_combine<T>(a, sh.d, s);
 }
 
@@ -1044,8 +1046,8 @@ void launch_weigh_decode(const Shape& sh, const LayerTable& chan_map, const Chan
   a.scores = scores;
   a.lse = lse;
   a.s_ld = weigh_ld(sh);
-  decode_states<T>(a, sh, G, nlive, s);
-  decode_combine<T>(a, sh.d, s);
+  decode_states<T>(a, sh, G, nlive, 0, s);
+  decode_combine<T, true>(a, sh.d, s);
   const dim3 grid((unsigned)((a.s_ld / 4 + 255) / 256), (unsigned)(sh.Hkv * sh.B * nlive));
   hipLaunchKernelGGL(decode_weigh_kernel<T>, grid, dim3(256), 0, s, a, weight);
 }
@@ -1079,10 +1081,12 @@ size_t decode_shared_bytes(const Shape& sh, int P) {
 template <int DH>
 static void shared_mfma(DecodeArgs<bf16>& a, const Reach& r, const PrefixPlan& p, int G, int nlive,
                         const Shape& sh, hipStream_t s) {
-  const DecodePlan d = decode_plan<DH>(a, G, nlive, sh);
+  const DecodePlan d = decode_plan<DH>(a, G, nlive, sh, p.nsplit);
   const int rows = 32 * p.rt * p.rw, z = (G * sh.B + rows - 1) / rows;
   const PrefixSpan px{(const bf16*)r.Kp, (const bf16*)r.Vp, r.P, r.P_cap, p.nsplit, p.split_len, z,
-                      z * p.nsplit * sh.Hkv * nlive, d.own, sh.Hkv * sh.B * nlive};
+                      z * p.nsplit * sh.Hkv * nlive, d.own, sh.Hkv * sh.B * nlive,
+                      a.part};
+  a.part += (long)p.nsplit * (DH + 2);
   const dim3 grid((unsigned)(px.blocks + (long)d.own * px.slices * d.z));
 #define WM_SHARED_GO(RW, RT)                                                                     \
   do {                                                                                           \
@@ -1109,7 +1113,7 @@ void launch_shared_decode(const Shape& sh, const Reach& r, const LayerTable& cha
   DecodeArgs<T> a = decode_args<T>(sh, chan_map, cg, Q, Kc, Vc, Kd, Vd, ctx_len, nullptr, partials,
                                    O, &nlive, &G);
   const PrefixPlan p = prefix_plan(sh, r.P);
-  a.split0 = r.P > 0 ? p.nsplit : 0;
+  const int more = r.P > 0 ? p.nsplit : 0;
   bool done = false;
   if constexpr (sizeof(T) == 2) {
     done = sh.d != 32 && r.P > 0;
@@ -1117,11 +1121,13 @@ void launch_shared_decode(const Shape& sh, const Reach& r, const LayerTable& cha
                          : shared_mfma<64>(a, r, p, G, nlive, sh, s);
   }
   if (!done) {
-    decode_states<T>(a, sh, G, nlive, s);
+    a.part = partials + (long)more * (sh.d + 2);
+    decode_states<T>(a, sh, G, nlive, more, s);
     if (r.P > 0)
       launch_prefix_rows<T>(sh, r, a.live, nlive, a.cg, G * sh.B, Q, partials, a.nsplit, p.nsplit,
                             p.split_len, s);
   }
+  a.part = partials;
   decode_combine<T>(a, sh.d, s);
 }
 

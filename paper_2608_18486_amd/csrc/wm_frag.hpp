@@ -82,9 +82,26 @@ __device__ __forceinline__ float pf_wsum(const bf16x8& a, const bf16x8& b) {
 }
 
 // 16 fp32 weights as three bf16 parts of 8 bits each, exact to 24: a weight's upper 16 bits are its
-// first part; twice more from what is left. What is left comes from a dot product of the pair just
-// cut with (-1, 0) or (0, -1), one instruction where masking the part out and subtracting are two.
+// first part; twice more from what is left.
 __device__ __forceinline__ void cut24(const f32x16& p, bf16x8 (&pw)[3][2]) {
+#pragma unroll
+  for (int q = 0; q < 16; q += 2) {
+    uint32_t r0 = __float_as_uint(p[q]), r1 = __float_as_uint(p[q + 1]);
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+      const bf16x2 w2 = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(r1, r0, 0x07060302u));
+      pw[u][q >> 3][q & 7] = w2[0];
+      pw[u][q >> 3][(q & 7) + 1] = w2[1];
+      r0 = __float_as_uint(__uint_as_float(r0) - __uint_as_float(r0 & 0xffff0000u));
+      r1 = __float_as_uint(__uint_as_float(r1) - __uint_as_float(r1 & 0xffff0000u));
+    }
+  }
+}
+// The same parts, what is left from a dot product of the pair just cut with (-1, 0) or (0, -1): one
+// instruction where masking the part out and subtracting are two. Faster where the vector
+// instructions of the cut stand between products (the window's gradients: 5%); decode, where
+// they follow each other at once, loses 3% to it.
+__device__ __forceinline__ void cut24_dot(const f32x16& p, bf16x8 (&pw)[3][2]) {
   // (kept in registers: as an immediate, 0xbf800000 is the inline constant -1.0, which the
   // instruction reads as (-1, 0) too)
   uint32_t clo = 0x0000bf80u, chi = 0xbf800000u;
