@@ -627,7 +627,7 @@ __global__ __launch_bounds__(256) void decode_weigh_kernel(DecodeArgs<T> a, floa
 // its own few rows. A workgroup's two waves share the blocks they read: either each has RT tiles of
 // 32 rows of its own (RW = 2), wave 0 copying K and wave 1 V into a ring of three blocks, or, where a
 // slice has 32 rows at most, both take the same rows and every second block (RW = 1, a ring of two
-// pairs). Scores and weights as in decode_block, the weights in 24 bits.
+// pairs). Scores as in decode_block, the weights in 17 bits.
 // The workgroups of a prefix's splits and those of the sequences' own caches (decode_block) form
 // one grid: the former are bound by their products and exponentials, the latter by the stream of the
 // cache, and a CU holds some of each at a time. (64 sequences, 24 layers of 16 heads of 64, 4096 + 300

@@ -97,30 +97,4 @@ __device__ __forceinline__ void cut24(const f32x16& p, bf16x8 (&pw)[3][2]) {
     }
   }
 }
-// The same parts, what is left from a dot product of the pair just cut with (-1, 0) or (0, -1): one
-// instruction where masking the part out and subtracting are two. Faster where the vector
-// instructions of the cut stand between products (the window's gradients: 5%); decode, where
-// they follow each other at once, loses 3% to it.
-__device__ __forceinline__ void cut24_dot(const f32x16& p, bf16x8 (&pw)[3][2]) {
-  // (kept in registers: as an immediate, 0xbf800000 is the inline constant -1.0, which the
-  // instruction reads as (-1, 0) too)
-  uint32_t clo = 0x0000bf80u, chi = 0xbf800000u;
-  asm("" : "+s"(clo), "+s"(chi));
-  const bf16x2 lo = __builtin_bit_cast(bf16x2, clo), hi = __builtin_bit_cast(bf16x2, chi);
-#pragma unroll
-  for (int q = 0; q < 16; q += 2) {
-    float r0 = p[q], r1 = p[q + 1];
-#pragma unroll
-    for (int u = 0; u < 3; ++u) {
-      const bf16x2 w2 = __builtin_bit_cast(
-          bf16x2, __builtin_amdgcn_perm(__float_as_uint(r1), __float_as_uint(r0), 0x07060302u));
-      pw[u][q >> 3][q & 7] = w2[0];
-      pw[u][q >> 3][(q & 7) + 1] = w2[1];
-      if (u < 2) {
-        r0 = __builtin_amdgcn_fdot2_f32_bf16(w2, lo, r0, false);
-        r1 = __builtin_amdgcn_fdot2_f32_bf16(w2, hi, r1, false);
-      }
-    }
-  }
-}
 }  // namespace wm

@@ -165,9 +165,5 @@ template <int Q0, int Q1> __device__ __forceinline__ float tree_sum(const f32x16
     return tree_sum<Q0, QM>(v) + tree_sum<QM, Q1>(v);
   }
 }
-template <int N, int I0 = 0> __device__ __forceinline__ float tree_sum_arr(const float* p) {
-  if constexpr (N == 1) return p[I0];
-  else return tree_sum_arr<N / 2, I0>(p) + tree_sum_arr<N - N / 2, I0 + N / 2>(p);
-}
 
 }  // namespace wm

@@ -6,13 +6,13 @@
 // Four steps:
 //   reach_bwd_dq_kernel    query-major: LSE, D and dq in one walk over the slots that the tile's
 //                          rows read, with an online maximum
-//   reach_bwd_dkv_kernel   slot-major: 128 slots of one (channel, sequence, KV head) against the
+//   reach_bwd_dkv_kernel   slot-major: 64 slots of one (channel, sequence, KV head) against the
 //                          rows whose windows hold them
 //   reach_bwd_sink_*       the first slots against the rows whose windows lie past them: all later
 //                          rows, which one slot tile would walk alone, cut over waves and
 //                          workgroups
 //   the dummy              as in wm_backward.hip
-// P and dS enter the products as three bf16 parts of 8 bits (cut24_dot), so that fp32 gradients keep
+// P and dS enter the products as three bf16 parts of 8 bits (cut24), so that fp32 gradients keep
 // fp32's digits: with one rounded part they are off by 2e-3 of themselves. That makes 13 products
 // of the formula's 5 (S and dP twice, dv, dk and dq three parts each) and as many vector
 // instructions for the parts as for the weights, which bounds the kernels.
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * kReachBwdWaves) void reach_bwd_dq_kernel(Reach
         }
         sum += ps[0] + ps[1];
         bf16x8 dw[3][2];
-        cut24_dot(ds, dw);
+        cut24(ds, dw);
 #pragma unroll
         for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
@@ -274,7 +274,7 @@ __device__ __forceinline__ void reach_bwd_rows(const char* sm, const PfLane<DH>&
     }
   }
   bf16x8 pw[3][2];
-  cut24_dot(sc, pw);
+  cut24(sc, pw);
 #pragma unroll
   for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
@@ -284,7 +284,7 @@ __device__ __forceinline__ void reach_bwd_rows(const char* sm, const PfLane<DH>&
       for (int u = 0; u < 3; ++u) dv[dt] = mma32(dv[dt], f, pw[u][kh]);
     }
   dp *= sc;
-  cut24_dot(dp, pw);
+  cut24(dp, pw);
 #pragma unroll
   for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
