@@ -800,14 +800,17 @@ void launch_dummy_backward(const Shape& sh, const ChannelGroups& groups, const b
   a.Q = Q, a.dO = dO, a.pd = pd, a.dsd = dsd, a.dKd = dKd, a.dVd = dVd;
   a.B = sh.B, a.T = sh.T_new, a.L = sh.L, a.Hq = sh.Hq, a.Hkv = sh.Hkv;
   a.mask_paper = sh.mask_paper, a.scale = 1.0f / sqrtf((float)sh.d);
-  a.grp = groups, a.dchunks = dummy_chunks(sh);
+  // (inclusive mask: no partial sums, and their sum writes the zeros)
+  a.grp = groups, a.dchunks = sh.mask_paper ? dummy_chunks(sh) : 0;
   const dim3 gp(sh.k * sh.Hkv * a.dchunks), gs(sh.k * sh.Hkv);
   if (sh.d == 64) {
-    hipLaunchKernelGGL(attend_bwd_dummy_part_kernel<64>, gp, dim3(4 * 64), 0, s, a, part);
+    if (a.dchunks > 0)
+      hipLaunchKernelGGL(attend_bwd_dummy_part_kernel<64>, gp, dim3(4 * 64), 0, s, a, part);
     hipLaunchKernelGGL(attend_bwd_dummy_sum_kernel<64>, gs, dim3(4 * 64), 0, s, a,
                        (const float*)part);
   } else {
-    hipLaunchKernelGGL(attend_bwd_dummy_part_kernel<96>, gp, dim3(4 * 96), 0, s, a, part);
+    if (a.dchunks > 0)
+      hipLaunchKernelGGL(attend_bwd_dummy_part_kernel<96>, gp, dim3(4 * 96), 0, s, a, part);
     hipLaunchKernelGGL(attend_bwd_dummy_sum_kernel<96>, gs, dim3(4 * 96), 0, s, a,
                        (const float*)part);
   }

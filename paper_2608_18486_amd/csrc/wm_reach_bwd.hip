@@ -581,8 +581,7 @@ constexpr int kSinkParts = 16;
 
 static size_t reach_rows(const Shape& sh) { return (size_t)sh.L * sh.N() * sh.Hq; }
 static size_t sink_part_floats(const Shape& sh) {
-  const size_t groups = std::min(kSinkParts, (sh.S_cap + 31) / 32 * kSinkParts);
-  return groups * sh.k * sh.B * sh.Hkv * 2 * 32 * sh.d;
+  return (size_t)kSinkParts * sh.k * sh.B * sh.Hkv * 2 * 32 * sh.d;
 }
 size_t reach_backward_bytes(const Shape& sh) {
   return (4 * reach_rows(sh) + sink_part_floats(sh)) * sizeof(float) + dummy_backward_bytes(sh);
