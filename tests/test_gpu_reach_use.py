@@ -44,8 +44,9 @@ def test_sequences_that_share_a_prefix(wm):
     """A prompt's cache laid out once; three sequences pool their own tokens at positions from 0
     and attend both. The same as attention over the whole: the same tokens pooled behind copies of
     the prompt, positions from the prompt's end, which the shared call sees only through RoPE's
-    relative positions (and a dummy turned to match). Keys and queries of either run are off by their fp32 rounding and by the
-    angle's (2^-21), of their size: scores by 6 2^-21 sigma more than a call's own bound."""
+    relative positions (and a dummy turned to match). Keys and queries of either run are off by
+    their fp32 rounding and by the angle's (2^-21), of their size: scores by 6 2^-21 sigma more
+    than a call's own bound."""
     n, own, T = 77, 40, 5
     P, dims, cmap = _model(wm, 3, 128, T, 100)
     g = torch.Generator().manual_seed(1)
