@@ -347,6 +347,18 @@ __device__ __forceinline__ void reach_tile(const ReachArgs<bf16>& a, const int t
   }
 }
 
+// The place of the t-th tile taken of a share of `count`, which lie head by head (or slice by slice)
+// with n tiles each, longest first: in that order, but the last heads that hold `last` tiles
+// give all their longest ones first, then the next ones, so that no long tile starts when the
+// others end. (All heads this way would read the K and V of all at once: 2 x 2048 tokens, 24 layers
+// of 16 heads of 64, no window, 530 us in order, 550 so. Four tiles per workgroup in the
+// last heads, in order / so: 2 x 1023 tokens of weighed attention 137 / 133, 4001 tokens of
+// 12 layers of 12 heads 379 / 366, under a window of 1024 215 / 211.)
+__device__ __forceinline__ int long_first(int t, int count, int n, int last) {
+  const int nb = min(count / n, (last + n - 1) / n), v = t - (count - nb * n);
+  return v < 0 ? t : t - v + v % nb * n + v / nb;
+}
+
 // Grid and work queue as the prefill kernel's (attend_prefill_dma_kernel): one workgroup per tile
 // where the CUs hold them all at once, else as many as they hold, each XCD's taking tiles of its
 // contiguous share from a counter (queue, reset on the stream before).
@@ -370,7 +382,9 @@ void reach_dma_kernel(ReachArgs<bf16> a, uint32_t* queue) {
   __syncthreads();
   int t = __builtin_amdgcn_readfirstlane(s_tile);
   while (t < count) {
-    reach_tile<DH, PRE, LSE>(a, first + t, smem);
+    // (a prefix's tiles are alike but for their own slots: no use in turning their order)
+    reach_tile<DH, PRE, LSE>(
+        a, first + (PRE ? t : long_first(t, count, a.n_qtiles, 4 * (int)(gridDim.x / nq))), smem);
     if (tid == 0) s_tile = (int)atomicAdd(ctr, 1u);
     __syncthreads();
     t = __builtin_amdgcn_readfirstlane(s_tile);
@@ -946,7 +960,7 @@ __global__ __launch_bounds__(256) void reach_weigh_kernel(ReachArgs<T> a, Channe
 // bf16 at head dims 64 and 96: the same with the query blocks copied into a ring of three in LDS per
 // wave (fragments loaded from memory touch 32 lines an instruction, which the CU's L1 looks up one
 // by one), two score sets in turn, and the slot tiles of a slice on one XCD, whose L2 then serves
-// its queries to all of them. 2 x 1023 tokens, 16 layers of 6/3 heads of 96: 62 us; with the tiles
+// its queries to all of them. 2 x 1023 tokens, 16 layers of 6/3 heads of 96: 62 us (51 with the long tiles of the last slices first); with the tiles
 // over the XCDs 81, from memory 77.
 template <int DH>
 __global__ __launch_bounds__(256) void reach_weigh_dma_kernel(ReachArgs<bf16> a, ChannelGroups cg,
@@ -958,7 +972,11 @@ __global__ __launch_bounds__(256) void reach_weigh_dma_kernel(ReachArgs<bf16> a,
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, r = lane & 31;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   // the slot tiles of a slice, which read the same queries, on one XCD
-  const int tile = xcd_tile(blockIdx.x, (int)gridDim.x), slice = tile / a.n_qtiles;
+  const int nq = min((int)gridDim.x, kNumXcd), share = (int)gridDim.x / nq;
+  int tile = xcd_tile(blockIdx.x, (int)gridDim.x);
+  if ((int)gridDim.x % nq == 0)
+    tile = tile / share * share + long_first(tile % share, share, a.n_qtiles, a.z);
+  const int slice = tile / a.n_qtiles;
   const int kvh = slice % a.Hkv, b = slice / a.Hkv % a.B, c = slice / a.Hkv / a.B;
   const int p0 = __builtin_amdgcn_readfirstlane(ctx_at(a.ctx_len, b, a.ctx_hi)) + a.gq +
                  (a.mask_paper ? 0 : 1);
@@ -1188,6 +1206,7 @@ void launch_weigh(const Shape& sh, const LayerTable& chan, const ChannelGroups& 
                                  const_cast<float*>(lse));
   const long most = (long)sh.ctx_max + sh.span();
   a.n_qtiles = (int)((most + 63) / 64);  // slot tiles of a slice
+  a.z = 4 * device_cus() / kNumXcd;      // tiles whose longest start first: two per place
   const dim3 grid((unsigned)((long)a.n_qtiles * sh.k * sh.B * sh.Hkv));
   if constexpr (sizeof(T) == 2) {
     if (sh.d == 96)
