@@ -515,7 +515,8 @@ int wm_prefix_share(const wm_dims *dims, const void *Kc, const void *Vc, int32_t
  * as given (wm_prefix_share turns it to match).
  *   prefix_len  0 <= prefix_len <= P_cap (0: Kp and Vp are not read and may be NULL)
  *   Kp, Vp      device [k][Hkv][P_cap][d] in dtype (see wm_prefix_share)
- * Few new tokens (T_new <= 4): the prefix is read once for the whole batch. Other arguments
+ * Few new tokens (T_new <= 4, up to 16 of many heads over a long prefix): the prefix is read once
+ * for the whole batch. Other arguments
  * and errors as wm_channel_attend; workspace: wm_shared_workspace(dims, prefix_len). */
 int wm_channel_attend_shared(const wm_dims *dims, const wm_params *params, const void *Q,
                              const int32_t *chan_map, const int32_t *ctx_len,

@@ -1216,9 +1216,27 @@ int check_prefix(const wm_dims& d, int32_t prefix_len, int32_t P_cap) {
   return WM_OK;
 }
 
+// Whether the batch's rows meet the prefix together (launch_shared_decode): always for few tokens, and
+// up to 16 where that saves more than the partial states cost. A head's own tile is padded to 32
+// rows, so it saves heads x prefix x (32 - T_new) products. us a call, tiles per head / this: 24
+// layers of 16 heads of 64, prefix 2000, 16 sequences of 5 / 16 / 24 tokens 215 / 226 / 226 and 127 /
+// 174 / 265, 64 sequences (6 channels) of 5 745 and 245; prefix 700, 16 of 16 105 and 111;
+// 12 of 12, 16 of 16 over 1000 53 and 63, 8 of 8 over 4000 90 and 62; 16 of 6/3 heads of 96, 4 of 8 over
+// 2000 29 and 41. In fp32, whose products cost more, 16 of 16 over 2000 / 700 1262 / 573 and
+// 879 / 549, 8 of 8 over 4000 562 and 164; but there (and at head dim 32) every four rows read their
+// own cache anew: 32 of 8 over 100 and their own 300 slots 253 and 370.
+bool prefix_together(const wm_dims& d, int32_t prefix_len) {
+  if (decode_path(d)) return true;
+  if (d.T_new > 16 || prefix_len == 0) return false;
+  const bool mfma = d.dtype == WM_BF16 && d.d != 32;
+  const double saved = (double)d.L * d.B * d.Hq * prefix_len * (32 - d.T_new);
+  return mfma ? saved >= 80e6
+              : saved >= 30e6 && prefix_len >= 4 * ((long long)d.ctx_max + call_span(d));
+}
+
 size_t shared_ws(const wm_dims& d, int32_t prefix_len) {
   if ((size_t)d.B * d.T_new == 0) return 0;
-  return al256(decode_path(d) ? wm::decode_shared_bytes(make_shape(d), prefix_len)
+  return al256(prefix_together(d, prefix_len) ? wm::decode_shared_bytes(make_shape(d), prefix_len)
                               : wm::kPrefillQueueBytes);
 }
 
@@ -1228,7 +1246,7 @@ void run_shared(const wm_dims& d, const wm_params& P, const wm::Reach& r, const 
                 void* ws, hipStream_t s) {
   const wm::Shape sh = reach_shape(d);
   const wm::LayerTable mt = map_table(d, chan_map);
-  if (decode_path(d))
+  if (prefix_together(d, r.P))
     wm::launch_shared_decode<T>(sh, r, mt, groups(d, chan_map), Q, Kc, Vc, (const T*)P.Kd,
                                 (const T*)P.Vd, ctx_len, (float*)ws, O, s);
   else

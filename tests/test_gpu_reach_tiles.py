@@ -146,6 +146,28 @@ def test_shared_scores_far_below_zero(wm, d, T):
             _close_out(c, r, O, "O")
 
 
+@pytest.mark.parametrize("dtype,d,T,ctx,P", [
+    ("bf16", 64, 5, 40, 1400), ("bf16", 96, 8, 0, 1500), ("bf16", 64, 16, 33, 2200),
+    ("f32", 64, 5, 40, 700), ("f32", 32, 16, 0, 830), ("bf16", 32, 8, 30, 550)])
+@pytest.mark.parametrize("paper", [True, False])
+def test_batch_of_short_questions(wm, dtype, d, T, ctx, P, paper):
+    """So many heads over so long a prefix that the batch's rows of 5 to 16 tokens meet it
+    together."""
+    B = 16
+    c = _make(39, L=12, B=B, T=T, Hq=12, Hkv=6, d=d, k=4, S=ctx + T + 2, dtype=dtype, P=P,
+              ctx=[ctx * b // (B - 1) for b in range(B)])
+    print("questions", dtype, d, T, ctx, P, paper, flush=True)
+    assert 12 * B * 12 * P * (32 - T) >= (80e6 if dtype == "bf16" and d != 32 else 30e6)
+    r = _oracle(c, paper)
+    c["Kp"][:, :, P:] = c["Vp"][:, :, P:] = float("nan")
+    _bury(c, paper)
+    dims, params, t, cl, O = _setup(wm, c, paper)
+    wm.channel_attend_shared(dims, params, t["Q"], c["map"], cl, P, t["Kp"], t["Vp"], t["Kc"],
+                             t["Vc"], O, ws=_ws(wm, wm.shared_workspace(dims, P)))
+    torch.cuda.synchronize()
+    _close_out(c, r, O, "O")
+
+
 def test_prefix_alone(wm):
     """Sequences with nothing of their own: in the paper's mask a first token reads the prefix
     and the dummy only."""
