@@ -523,7 +523,8 @@ int wm_channel_attend_shared(const wm_dims *dims, const wm_params *params, const
                              int32_t prefix_len, int32_t P_cap, const void *Kp, const void *Vp,
                              const void *Kc, const void *Vc, void *O, void *ws, size_t ws_bytes,
                              wm_stream_t stream);
-/* Bytes of workspace wm_channel_attend_shared needs; 0 when dims are invalid or
+/* Bytes of workspace wm_channel_attend_shared needs for these dims and this prefix_len (a shorter
+ * prefix or context may need more, where it is cut otherwise); 0 when dims are invalid or
  * prefix_len < 0. */
 size_t wm_shared_workspace(const wm_dims *dims, int32_t prefix_len);
 
